@@ -1,0 +1,399 @@
+"""The 8-bit cache and the token window as measurable cases, beside their plain forms.
+
+Three operators over the paged K/V cache of ``paper_2607_04443_amd.ws``:
+
+  append  ``Cache.append_many`` into a cache held in 8 bits: keys normed, rotated
+          and quantised on the way, values quantised, with one scale for each
+          64-token block and head; ``Cache.gather`` reads the segments back
+  attend  ``Cache.unit_attention`` / ``Cache.audio_attention`` over such a cache
+  window  ``Cache.window_attention``: each row sees the last ``window`` tokens of
+          the timeline and its first ``sinks`` tokens, over a cache of any format
+
+The 8-bit formats, for a block with largest magnitude a (codes q, values q s):
+  int8  s = a / 127 in fp32, at least 2^-126;  q = x / s to the nearest, ties to even
+  e4m3  s = 2^e, e >= -126 the least with a <= 448 2^e;  q = x / s rounded to e4m3
+"""
+import math
+
+import torch
+
+own = False
+
+D = 128
+PAGE = 64
+PAIRS = (22, 21, 21)  # rotary pairs driven by t, h, w
+THETA = 10000.0
+EPS = 1e-6
+LOG2E = 1.4426950408889634
+COND, VIDEO, AUDIO = 0, 1, 2
+
+
+# --------------------------------------------------------------------------- #
+# cases
+# --------------------------------------------------------------------------- #
+def _case(op, fmt, heads, cond, units, video, audio, name=None, **extra):
+    """A timeline of one conditioning slice and ``units`` units of ``video`` and
+    ``audio`` tokens (0: none)."""
+    c = {"op": op, "format": fmt, "heads": heads, "cond": cond, "units": units, "video": video, "audio": audio,
+         "cols": 40}
+    c.update(extra)
+    if name:
+        c["name"] = name
+    return c
+
+
+def listed():
+    return [
+        # smallest append: the 4 audio tokens of a 12-head stream's unit
+        _case("append", "int8", 12, 0, 1, 0, 4, name="append_audio"),
+        # a denoising step of the 640x368 stream: slice, video and audio K/V
+        _case("append", "e4m3", 40, 256, 1, 920, 4, name="append_step"),
+        # a refill after a stall: eight units of an odd token count at once
+        _case("append", "int8", 40, 101, 8, 917, 0, name="append_units"),
+        # odd head, token and slice counts, queries normed in the call
+        _case("attend", "int8", 17, 101, 6, 333, 3, rows=333, mode="norm_rope", cols=37, name="attend_ragged"),
+        # the 640x368 stream's 4 audio tokens over its 8-unit window
+        _case("attend", "e4m3", 40, 336, 9, 920, 4, rows=4, mode="norm_rope", few=True, name="attend_audio"),
+        # its 920 video tokens over the same window, queries prepared first
+        _case("attend", "e4m3", 40, 256, 9, 920, 0, rows=920, mode="prepared", name="attend_hist8"),
+        # and over the long one, 32 units of history
+        _case("attend", "int8", 40, 256, 33, 920, 0, rows=920, mode="prepared", name="attend_hist32"),
+        # smallest call: one new token over a short stream
+        _case("window", "bf16", 12, 64, 3, 252, 0, rows=1, mode="raw", window=256, sinks=4, causal=True,
+              cols=21, name="window_one"),
+        # a unit's 4 audio tokens over the audio tokens of 200 units alone
+        _case("window", "int8", 40, 0, 200, 0, 4, rows=4, mode="norm_rope", window=512, sinks=16, causal=True,
+              name="window_audio"),
+        # 4 tokens over the long stream: a wide window, the slice as sinks
+        _case("window", "e4m3", 40, 256, 33, 920, 0, rows=4, mode="norm_rope", window=8192, sinks=256,
+              causal=True, name="window_long"),
+        # a unit that sees itself both ways, four units back and the slice
+        _case("window", "bf16", 40, 256, 9, 920, 0, rows=920, mode="prepared", window=3680, sinks=256,
+              causal=False, name="window_unit"),
+        # a long run of tokens at once, each over its own last 1024
+        _case("window", "int8", 12, 256, 8, 512, 0, rows=4096, mode="prepared", window=1024, sinks=64,
+              causal=True, name="window_run"),
+    ]
+
+
+def draw(rng):
+    def log_int(lo, hi):
+        return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+    while True:
+        op = rng.choices(["append", "attend", "window"], [2, 3, 4])[0]
+        fmt = rng.choice(["int8", "e4m3"] if op != "window" else ["bf16", "int8", "e4m3"])
+        heads = rng.choice([12, 40, rng.randint(1, 40)])
+        cond = rng.choice([0, 256, log_int(1, 512)])
+        if op == "append":
+            units = rng.randint(1, 7)
+            c = _case(op, fmt, heads, cond, units, log_int(1, 1024), rng.choice([0, 4, log_int(1, 64)]))
+        else:
+            c = _case(op, fmt, heads, cond, log_int(1, 33), log_int(24, 1024), rng.choice([0, 4, log_int(1, 16)]))
+            if rng.random() < 0.1:  # an audio-only timeline
+                c["units"], c["video"], c["audio"] = log_int(1, 256), 0, rng.randint(1, 8)
+            c["mode"] = rng.choice(["norm_rope", "prepared", "raw"])
+            if op == "attend":
+                c["few"] = c["video"] == 0 or rng.random() < 0.4
+                c["rows"] = log_int(1, 64) if c["few"] else c["video"]
+            else:
+                n = sum(_lengths(c))
+                c["rows"] = min(rng.choice([1, log_int(1, 64), c["video"] or 1, log_int(64, 4096)]), n)
+                c["window"], c["sinks"] = log_int(1, 8192), rng.choice([0, 4, log_int(1, 512)])
+                c["causal"] = rng.random() < 0.7
+        c["cols"] = rng.randint(16, 64)
+        w = work(c)
+        if w["flops"] <= 5.8e11 and w["bytes"] <= 7.2e8 and heads * sum(_lengths(c)) <= 1300000:
+            return c  # no dearer than the largest listed ones
+
+
+def _segments(c):
+    """(unit, kind, tokens) along the timeline."""
+    seg = [(0, COND, c["cond"])]
+    seg += [(u, kind, n) for u in range(c["units"]) for kind, n in ((VIDEO, c["video"]), (AUDIO, c["audio"]))]
+    return [s for s in seg if s[2] > 0]
+
+
+def _lengths(c):
+    return [n for _, _, n in _segments(c)]
+
+
+def _seen(c):
+    """Tokens of the timeline that the call's kinds take in: a unit's video rows
+    do not see audio tokens."""
+    if c["op"] == "attend" and not c.get("few"):
+        return c["cond"] + c["units"] * c["video"]
+    return sum(_lengths(c))
+
+
+def _pairs(c):
+    """Visible (row, key) pairs of a head."""
+    n, rows = _seen(c), c["rows"]
+    if c["op"] == "attend":
+        return rows * n
+    t = torch.arange(n - rows, n, dtype=torch.int64)
+    hi = t + 1 if c["causal"] else torch.full_like(t, n)
+    lo = (t + 1 - c["window"]).clamp(min=0)
+    return int((hi - lo + torch.minimum(lo, torch.full_like(lo, c["sinks"]))).sum())
+
+
+def work(case):
+    c, H = case, case["heads"]
+    row = H * D  # elements of one token of K, V, Q or O
+    if c["op"] == "append":
+        n = sum(_lengths(c))  # K and V in, codes and scales stored, K and V out
+        scales = 8.0 * H * sum(-(-x // PAGE) for x in _lengths(c))
+        return {"bytes": 2 * n * row * (2 + 1 + 2) + scales, "flops": 20.0 * n * row}
+    cell = 2 if c["format"] == "bf16" else 1
+    n, rows = _seen(c), c["rows"]
+    if c["op"] == "window":  # tokens that some row sees
+        lo = max(0, n - rows + 1 - c["window"])
+        n = n - lo + min(lo, c["sinks"])
+    return {"bytes": 2.0 * n * row * cell + 4.0 * rows * row, "flops": 4.0 * row * _pairs(c)}
+
+
+# --------------------------------------------------------------------------- #
+# inputs
+# --------------------------------------------------------------------------- #
+def _positions(c, segs):
+    """(t, h, w) of every token of the segments, in order."""
+    n = torch.tensor([s[2] for s in segs], device="cuda")
+    unit = torch.tensor([s[0] for s in segs], device="cuda").repeat_interleave(n)
+    kind = torch.tensor([s[1] for s in segs], device="cuda").repeat_interleave(n)
+    i = torch.arange(int(n.sum()), device="cuda") - (n.cumsum(0) - n).repeat_interleave(n)
+    audio = kind == AUDIO
+    h = torch.where(audio, torch.zeros_like(i), i // c["cols"])
+    w = torch.where(audio, i, i % c["cols"])
+    return torch.stack([unit, h, w], dim=1).to(torch.int32).contiguous()
+
+
+def _inputs(case, seed):
+    """All values of a case, from the seed alone."""
+    c, H = case, case["heads"]
+    g = torch.Generator(device="cuda").manual_seed(1000003 * (seed + 1) + 11)
+
+    def normal(n):
+        return torch.randn(n, H, D, generator=g, device="cuda", dtype=torch.float32)
+
+    def gamma():
+        return (1 + 0.1 * torch.randn(D, generator=g, device="cuda")).to(torch.bfloat16).float()
+
+    segs = _segments(c)
+    n = sum(s[2] for s in segs)
+    x = {"segs": segs, "gamma": gamma(), "v": normal(n).to(torch.bfloat16)}
+    k = normal(n)
+    # what a cache's history holds has been normed already
+    x["k"] = (k if c["op"] == "append" else k * torch.rsqrt(k.square().mean(-1, keepdim=True))).to(torch.bfloat16)
+    x["pos"] = _positions(c, segs)
+    if c["op"] != "append":
+        q = normal(c["rows"])
+        x["q"] = q.to(torch.bfloat16)
+        last = AUDIO if c.get("few") or not c["video"] else VIDEO
+        x["qpos"] = _positions(c, [(c["units"] - 1, last, c["rows"])])
+        x["qpos"][:, 1:].clamp_(max=127)
+    return x
+
+
+def prepare(case, seed):
+    c, x = case, _inputs(case, seed)
+    s = {"case": c, "x": x}
+    empty = dict(dtype=torch.bfloat16, device="cuda")
+    if c["op"] == "append":
+        s["k_out"], s["v_out"] = torch.empty(x["k"].shape, **empty), torch.empty(x["v"].shape, **empty)
+    else:
+        s["out"], s["qp"] = torch.empty(x["q"].shape, **empty), torch.empty(x["q"].shape, **empty)
+        # the tokens that the call's kinds take in
+        n = torch.tensor(_lengths(c), device="cuda")
+        kind = torch.tensor([t[1] for t in x["segs"]], device="cuda").repeat_interleave(n)
+        s["seen"] = kind != AUDIO if c["op"] == "attend" and not c.get("few") else kind >= 0
+    s["page"], s["n_pages"] = _page_of(c)
+    if own:
+        _fill(s)
+    elif c["op"] != "append" and c["format"] != "bf16":
+        # the cache a user keeps: codes and scales
+        s["kc"], s["ks"] = _quantise(x["k"].float(), s["page"], s["n_pages"], c["format"])
+        s["vc"], s["vs"] = _quantise(x["v"].float(), s["page"], s["n_pages"], c["format"])
+    torch.cuda.synchronize()
+    return s
+
+
+def _fill(s):
+    """The handle a user's program keeps: a cache, with the history in it."""
+    from paper_2607_04443_amd import ws
+    c, x = s["case"], s["x"]
+    s["ws"] = ws
+    s["cache"] = cache = ws.Cache(c["heads"], s["n_pages"], max_q_tokens=max(64, c.get("rows", 1)),
+                                  rope_max_pos=(512, 128, 1024), rope_pairs=PAIRS, rope_theta=THETA,
+                                  kv_format=c["format"])
+    kinds = {COND: ws.WS_KIND_COND, VIDEO: ws.WS_KIND_VIDEO, AUDIO: ws.WS_KIND_AUDIO}
+    at, items = 0, []
+    for unit, kind, n in x["segs"]:
+        it = dict(unit=unit, kind=kinds[kind], k=x["k"][at:at + n], v=x["v"][at:at + n])
+        if c["op"] == "append":
+            if kind != COND:
+                it.update(mode=ws.WS_APPEND_NORM_ROPE, positions=x["pos"][at:at + n], gamma=x["gamma"], eps=EPS)
+            items.append((it, dict(unit=unit, kind=kinds[kind], k_out=s["k_out"][at:at + n],
+                                   v_out=s["v_out"][at:at + n])))
+        else:
+            cache.append(**it)
+        at += n
+    s["items"] = [a for a, _ in items]
+    s["back"] = [b for _, b in items]
+    if c["op"] == "append":
+        return
+    unit = c["units"] - 1
+    seen = (ws.WS_KIND_COND, ws.WS_KIND_VIDEO, ws.WS_KIND_AUDIO)
+    if c["op"] == "attend":
+        few = c.get("few")
+        s["mask"] = ws.mask_spec(unit, kinds=seen if few else seen[:2])
+        s["call"] = cache.audio_attention if few else cache.unit_attention
+    else:
+        s["mask"] = ws.window_spec(unit, c["window"], c["sinks"], causal=c["causal"], kinds=seen)
+        s["call"] = cache.window_attention
+
+
+# --------------------------------------------------------------------------- #
+# one pass
+# --------------------------------------------------------------------------- #
+def run(state):
+    s, c, x = state, state["case"], state["x"]
+    if own:
+        ws, cache = s["ws"], s["cache"]
+        if c["op"] == "append":
+            cache.append_many(s["items"])
+            cache.gather(s["back"])
+            return [s["k_out"], s["v_out"]]
+        rope = dict(positions=x["qpos"], gamma=x["gamma"], eps=EPS)
+        if c["mode"] == "prepared":
+            cache.step_append(queries=[dict(q=x["q"], q_out=s["qp"], mode=ws.WS_APPEND_NORM_ROPE, **rope)])
+            s["call"](s["qp"], s["out"], s["mask"], ws.WS_QUERY_PREPARED)
+        elif c["mode"] == "norm_rope":
+            s["call"](x["q"], s["out"], s["mask"], ws.WS_APPEND_NORM_ROPE, **rope)
+        else:
+            s["call"](x["q"], s["out"], s["mask"], ws.WS_APPEND_RAW)
+        return [s["out"]]
+    if c["op"] == "append":
+        raw = torch.zeros(x["k"].shape[0], dtype=torch.bool, device="cuda")
+        raw[:c["cond"]] = True
+        k = torch.where(raw[:, None, None], x["k"].float(), _norm_rope(x["k"], x["pos"], x["gamma"]))
+        outs = []
+        for t in (k, x["v"].float()):
+            codes, scales = _quantise(t, s["page"], s["n_pages"], c["format"])
+            outs.append(_values(codes, scales, s["page"]).to(torch.bfloat16))
+        return outs
+    if c["format"] == "bf16":
+        k, v = x["k"].float(), x["v"].float()
+    else:
+        k, v = _values(s["kc"], s["ks"], s["page"]), _values(s["vc"], s["vs"], s["page"])
+    if _seen(c) < k.shape[0]:
+        k, v = k[s["seen"]], v[s["seen"]]
+    q = x["q"].float() if c["mode"] == "raw" else _norm_rope(x["q"], x["qpos"], x["gamma"])
+    logits = torch.matmul(q.transpose(0, 1).contiguous(), k.permute(1, 2, 0).contiguous()) / math.sqrt(D)
+    if c["op"] == "window":
+        n, rows = k.shape[0], q.shape[0]
+        t = torch.arange(n - rows, n, device="cuda")[:, None]
+        j = torch.arange(n, device="cuda")[None, :]
+        see = (j > t - c["window"]) | (j < c["sinks"])
+        logits = torch.where(see & (j <= t) if c["causal"] else see, logits, -math.inf)
+    p = torch.exp(logits - logits.amax(-1, keepdim=True))
+    p = p / p.sum(-1, keepdim=True)
+    return [torch.matmul(p, v.transpose(0, 1).contiguous()).transpose(0, 1).to(torch.bfloat16).contiguous()]
+
+
+# --------------------------------------------------------------------------- #
+# the plain forms' parts
+# --------------------------------------------------------------------------- #
+def _page_of(c):
+    """The 64-token block of every token (a segment starts a block), and their number."""
+    n = torch.tensor(_lengths(c), device="cuda")
+    blocks = (n + PAGE - 1) // PAGE
+    first = (blocks.cumsum(0) - blocks).repeat_interleave(n)
+    i = torch.arange(int(n.sum()), device="cuda") - (n.cumsum(0) - n).repeat_interleave(n)
+    return first + i // PAGE, int(blocks.sum())
+
+
+def _norm_rope(x, pos, gamma):
+    x = x.float()
+    x = x * torch.rsqrt(x.square().mean(-1, keepdim=True) + EPS) * gamma
+    freq = torch.cat([THETA ** (-torch.arange(n, dtype=torch.float64, device="cuda") / n) for n in PAIRS])
+    band = torch.tensor([0] * PAIRS[0] + [1] * PAIRS[1] + [2] * PAIRS[2], device="cuda")
+    ang = pos.double()[:, band] * freq  # 64 bits: angles of far positions
+    cos, sin = ang.cos().float()[:, None, :], ang.sin().float()[:, None, :]
+    a, b = x[..., 0::2], x[..., 1::2]
+    return torch.stack([a * cos - b * sin, a * sin + b * cos], dim=-1).flatten(-2)
+
+
+def _quantise(x, page, n_pages, fmt):
+    """Codes of [tokens, heads, 128] values, and the scale of each block and head."""
+    a = torch.zeros(n_pages, x.shape[1], device="cuda").index_reduce_(0, page, x.abs().amax(-1), "amax")
+    if fmt == "int8":
+        s = (a / 127).clamp(min=2.0 ** -126)
+        # 64 bits: a quotient next to a border
+        q = torch.round(x.double() / s[page][..., None].double()).clamp(-127, 127).to(torch.int8)
+        return q, s
+    m, e = torch.frexp(a)  # a = m 2^e, m in [0.5, 1); 448 = 0.875 * 2^9
+    e = (e - 9 + (m > 0.875).int()).clamp(min=-126)
+    s = torch.ldexp(torch.ones_like(a), torch.where(a > 0, e, torch.full_like(e, -126)))
+    return (x / s[page][..., None]).to(torch.float8_e4m3fn), s
+
+
+def _values(codes, scales, page):
+    return codes.float() * scales[page][..., None]
+
+
+# --------------------------------------------------------------------------- #
+# the same values in 64 bits, from the definitions
+# --------------------------------------------------------------------------- #
+def exact(case, seed):
+    c, x = case, _inputs(case, seed)
+
+    def rotate(t, pos):
+        t = t.double()
+        t = t / torch.sqrt((t * t).mean(-1, keepdim=True) + EPS) * x["gamma"].double()
+        ang = torch.cat([pos[:, b:b + 1].double() * THETA ** (-torch.arange(n, dtype=torch.float64, device="cuda") / n)
+                         for b, n in enumerate(PAIRS)], dim=1)[:, None, :]
+        z = torch.view_as_complex(t.unflatten(-1, (D // 2, 2)).contiguous()) * torch.polar(torch.ones_like(ang), ang)
+        return torch.view_as_real(z).flatten(-2)
+
+    def held(t):
+        """What the cache stands for, block by block."""
+        if c["format"] == "bf16":
+            return t.double()
+        out, at = torch.empty_like(t, dtype=torch.float64), 0
+        for n in _lengths(c):
+            for lo in range(at, at + n, PAGE):
+                b = t[lo:min(lo + PAGE, at + n)].double()
+                a = b.abs().amax((0, 2), keepdim=True)
+                if c["format"] == "int8":
+                    s = (a / 127).float().double().clamp(min=2.0 ** -126)
+                    q = torch.round(b / s).clamp(-127, 127)
+                else:
+                    s = torch.exp2(torch.ceil(torch.log2(a.clamp(min=2.0 ** -140) / 448)).clamp(min=-126))
+                    y = b / s
+                    step = torch.exp2(torch.floor(torch.log2(y.abs().clamp(min=2.0 ** -6))) - 3)
+                    q = (torch.round(y / step) * step).clamp(-448, 448)
+                out[lo:lo + b.shape[0]] = q * s
+            at += n
+        return out
+
+    if c["op"] == "append":
+        k = x["k"].double()
+        k[c["cond"]:] = rotate(x["k"][c["cond"]:], x["pos"][c["cond"]:])
+        return [held(k), held(x["v"])]
+    k, v = held(x["k"]), held(x["v"])
+    if c["op"] == "attend" and not c.get("few"):
+        keep = torch.cat([torch.full((n,), kind != AUDIO) for _, kind, n in x["segs"]]).to(k.device)
+        k, v = k[keep], v[keep]
+    q = x["q"].double() if c["mode"] == "raw" else rotate(x["q"], x["qpos"])
+    out, n, rows = torch.empty_like(q), k.shape[0], q.shape[0]
+    for h in range(c["heads"]):
+        s = q[:, h] @ k[:, h].t().contiguous() / math.sqrt(D)
+        if c["op"] == "window":
+            j = torch.arange(n, device=s.device).expand(rows, n)
+            back = torch.arange(n - rows, n, device=s.device)[:, None] - j  # tokens the key lies back
+            hidden = (back >= c["window"]) & (j >= c["sinks"])
+            if c["causal"]:
+                hidden |= back < 0
+            s = s.masked_fill(hidden, -math.inf)
+        out[:, h] = torch.softmax(s, -1) @ v[:, h]
+    return [out]
