@@ -10,7 +10,8 @@ Three operators over the paged K/V cache of ``paper_2607_04443_amd.ws``:
           the timeline and its first ``sinks`` tokens, over a cache of any format
 
 The 8-bit formats, for a block with largest magnitude a (codes q, values q s):
-  int8  s = a / 127 in fp32, at least 2^-126;  q = x / s to the nearest, ties to even
+  int8  s = a / 127 in fp32, rounded up to 16 significant bits, at least 2^-126
+        (q s is exact in fp32);  q = x / s to the nearest, ties to even
   e4m3  s = 2^e, e >= -126 the least with a <= 448 2^e;  q = x / s rounded to e4m3
 """
 import math
@@ -328,6 +329,7 @@ def _quantise(x, page, n_pages, fmt):
     a = torch.zeros(n_pages, x.shape[1], device="cuda").index_reduce_(0, page, x.abs().amax(-1), "amax")
     if fmt == "int8":
         s = (a / 127).clamp(min=2.0 ** -126)
+        s = ((s.view(torch.int32) + 255) & -256).view(torch.float32)
         # 64 bits: a quotient next to a border
         q = torch.round(x.double() / s[page][..., None].double()).clamp(-127, 127).to(torch.int8)
         return q, s
@@ -366,6 +368,8 @@ def exact(case, seed):
                 a = b.abs().amax((0, 2), keepdim=True)
                 if c["format"] == "int8":
                     s = (a / 127).float().double().clamp(min=2.0 ** -126)
+                    unit = torch.exp2(torch.floor(torch.log2(s)) - 15)
+                    s = torch.ceil(s / unit) * unit
                     q = torch.round(b / s).clamp(-127, 127)
                 else:
                     s = torch.exp2(torch.ceil(torch.log2(a.clamp(min=2.0 ** -140) / 448)).clamp(min=-126))
