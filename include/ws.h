@@ -98,6 +98,21 @@ typedef struct ws_cache_config {
   double rope_theta;       /* rotary base (> 1), e.g. 10000 */
 } ws_cache_config;
 
+/* How a cache holds its keys and values (ws_cache_create_format).  In 8 bits
+ * a 64-token page holds, for each head and for K and V, 64 x 128 codes and one
+ * fp32 scale; value = code * scale.  With a = the largest magnitude of the
+ * page's tokens of that head:
+ *   INT8: scale = a / 127 in fp32, rounded up to 16 significant bits, at least
+ *         2^-126; code = value / scale to the nearest integer, ties to even
+ *         (about 0.9% of the values' rms on normal values);
+ *   E4M3: scale = the least power of two >= 2^-126 with a <= 448 scale; code =
+ *         value / scale rounded to e4m3 (1 sign, 4 exponent, 3 fraction bits).
+ * Keys are normed and rotated in fp32 and rounded once, to the code.  An
+ * infinity, a NaN and, for INT8, a magnitude of 2^118 or more is stored as 0 and
+ * flagged (ws_cache_check, bit 1).  The attention reads code * scale rounded to
+ * bf16. */
+typedef enum ws_kv_format { WS_KV_BF16 = 0, WS_KV_INT8 = 1, WS_KV_E4M3 = 2 } ws_kv_format;
+
 typedef struct ws_append_desc {
   int32_t unit;              /* streaming unit the tokens belong to */
   ws_kind kind;
@@ -192,6 +207,17 @@ typedef enum ws_option {
  * On success *out owns all of it until ws_cache_destroy. */
 WS_API ws_status ws_cache_create(const ws_cache_config* cfg, ws_cache** out);
 
+/* ws_cache_create for a cache whose pools hold `format` (WS_KV_BF16 is
+ * ws_cache_create).  An 8-bit cache takes every call that a bf16 cache takes, in
+ * half the memory: pools of 2 * max_pages * H * 64 * 128 bytes and two fp32
+ * scales per (page, head).  Its appends quantise on the way, its attention calls
+ * read 8-bit pages; rows never ride in the video kernel (ws_step_attention runs
+ * the two calls' kernels). */
+WS_API ws_status ws_cache_create_format(const ws_cache_config* cfg, ws_kv_format format, ws_cache** out);
+
+/* The format a cache was created with.  Host-only. */
+WS_API ws_status ws_cache_format(const ws_cache* cache, ws_kv_format* format);
+
 /* Waits for the device, then frees everything the cache owns.  NULL is a no-op. */
 WS_API ws_status ws_cache_destroy(ws_cache* cache);
 
@@ -239,6 +265,27 @@ WS_API ws_status ws_kv_append_many(ws_cache* cache, int32_t n, const ws_append_i
  * read before the call returns (either may be NULL when its count is 0). */
 WS_API ws_status ws_step_append(ws_cache* cache, int32_t n_kv, const ws_append_item* kv,
                                 int32_t n_q, const ws_query_item* qs, void* hip_stream);
+
+/* One segment of a ws_kv_gather call: k_out and v_out are device bf16
+ * [n_tokens][H][128] with strides (tok_stride, head_stride), n_tokens the
+ * segment's; one of them may be NULL. */
+typedef struct ws_gather_item {
+  int32_t unit;
+  ws_kind kind;
+  void* k_out;
+  void* v_out;
+  int64_t tok_stride;
+  int64_t head_stride;
+} ws_gather_item;
+
+/* Reads n (1..WS_MAX_APPEND_ITEMS) segments out of the cache, in token order, to
+ * device memory: the stored bf16 values, or code * scale rounded to bf16 (what
+ * the attention of an 8-bit cache reads), e.g. to hand a slice on or to refill a
+ * cache of another format.  One launch per 8 items and 192 pages.  All items are
+ * checked before anything is enqueued (WS_ERR_UNKNOWN_UNIT for an absent
+ * segment; two items may name the same one).  The outputs must not overlap each
+ * other.  items: host array, read before the call returns. */
+WS_API ws_status ws_kv_gather(ws_cache* cache, int32_t n, const ws_gather_item* items, void* hip_stream);
 
 /* Marks the VIDEO and AUDIO segments of `unit` as committed history
  * (Sec. 2.1); they can no longer be rewritten.  Host-only. */
@@ -309,6 +356,36 @@ WS_API ws_status ws_audio_attention(const void* q, int64_t q_tok_stride, int64_t
                              int32_t n_q, const ws_query_desc* qdesc, ws_cache* cache,
                              const ws_mask_spec* mask, void* out, int64_t out_tok_stride,
                              int64_t out_head_stride, void* hip_stream);
+
+/* Attention under a token window with sinks: each row sees the last tokens
+ * before it and the first tokens of the stream.  The tokens that `mask` leaves
+ * visible, ordered by unit, then kind (COND, VIDEO, AUDIO), then position in
+ * their segment, are the timeline, indices 0 .. n - 1.  Row i of the call sits
+ * at index t = q_start + i and sees key j iff
+ *   (j > t - window  or  j < n_sink)  and, if causal, j <= t.
+ * So a causal row sees the `window` tokens that end with its own, and the first
+ * n_sink; without causal, everything after it as well (a unit that sees itself
+ * both ways, over a window of history).  A row that sees nothing gets a zero
+ * output. */
+typedef struct ws_window_spec {
+  ws_mask_spec mask;
+  int32_t window;    /* >= 1; 0: no window (every earlier token) */
+  int32_t n_sink;    /* >= 0 */
+  int32_t causal;    /* 0 or 1 */
+  int32_t q_start;   /* 0 .. 2^24, or WS_WINDOW_AT_END: the rows are the timeline's last n_q
+                        (where n < n_q, the first n_q - n rows lie before it) */
+} ws_window_spec;
+
+#define WS_WINDOW_AT_END (-1)
+
+/* Arguments as ws_unit_attention, 1 <= n_q <= max_q_tokens, over a cache of any
+ * format.  Only pages that some row sees are read.  The timeline may hold at most
+ * 2^24 tokens (WS_ERR_SHAPE).  A page list of more than 384 pages is uploaded, which a
+ * capturing stream refuses (WS_ERR_UNSUPPORTED).  Values of any kind in tokens
+ * that a row does not see, infinities and NaN included, do not reach it. */
+WS_API ws_status ws_window_attention(const void* q, int64_t q_tok_stride, int64_t q_head_stride, int32_t n_q,
+                                     const ws_query_desc* qdesc, ws_cache* cache, const ws_window_spec* window,
+                                     void* out, int64_t out_tok_stride, int64_t out_head_stride, void* hip_stream);
 
 /* One attention call of ws_step_attention: the arguments of
  * ws_unit_attention / ws_audio_attention. */
@@ -443,10 +520,16 @@ typedef struct ws_block_step_args {
 WS_API ws_status ws_block_step(ws_block* block, const ws_block_step_args* args, void* hip_stream);
 
 /* Debug read-back of one segment in logical order: k_host and v_host receive
- * bf16 [n_tokens][H][128] (contiguous host buffers owned by the caller).
- * Waits for the device.  k_host or v_host may be NULL to skip it. */
+ * bf16 [n_tokens][H][128] (contiguous host buffers owned by the caller); for an
+ * 8-bit cache code * scale rounded to bf16.  Waits for the device.  k_host or v_host may be NULL to skip it. */
 WS_API ws_status ws_cache_export(ws_cache* cache, int32_t unit, ws_kind kind, void* k_host,
                           void* v_host);
+
+/* The same for an 8-bit cache's own contents: codes [n_tokens][H][128] (int8, or
+ * the bits of e4m3) and scales fp32 [ceil(n_tokens / 64)][H].  Any of the four
+ * may be NULL.  WS_ERR_UNSUPPORTED for a bf16 cache. */
+WS_API ws_status ws_cache_export_codes(ws_cache* cache, int32_t unit, ws_kind kind, uint8_t* k_codes,
+                                       uint8_t* v_codes, float* k_scales, float* v_scales);
 
 /* Token count of a segment (WS_ERR_UNKNOWN_UNIT if absent). */
 WS_API ws_status ws_segment_tokens(ws_cache* cache, int32_t unit, ws_kind kind, int32_t* n_tokens);
@@ -462,7 +545,8 @@ WS_API ws_status ws_segment_pages(ws_cache* cache, int32_t unit, ws_kind kind, i
 WS_API ws_status ws_cache_info(ws_cache* cache, ws_cache_stats* stats);
 
 /* Waits for the device and returns (and clears) the device-side flags:
- * bit 0 = a position outside [0, rope_max_pos) was clamped. */
+ * bit 0 = a position outside [0, rope_max_pos) was clamped; bit 1 = an append to
+ * an 8-bit cache met a value that it does not hold (ws_kv_format; stored as 0). */
 WS_API ws_status ws_cache_check(ws_cache* cache, uint32_t* flags);
 
 /* Sets a tuning knob (see ws_option); value 0 restores the automatic choice. */
@@ -484,7 +568,7 @@ typedef struct ws_call_timing {
   int32_t path;      /* 0 = video attention, 1 = audio attention, 2 = append,
                         3 = QKV projection, 4 = output projection (ws_block_step),
                         5 = audio attention with its rows in the video kernel
-                        (ws_step_attention) */
+                        (ws_step_attention), 6 = window attention, 7 = gather */
   int32_t n_splits;  /* audio: key-range splits; video: workgroup groups; append: items */
   float attn_us;     /* attention kernel, microseconds */
   float merge_us;    /* merge kernel, microseconds (0 when there is none) */

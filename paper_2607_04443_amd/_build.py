@@ -1,7 +1,8 @@
 """Build of the native libraries, in-tree.
 
-  libws.so       the product: HIP kernels for gfx950 (kernels.hip; peaks.hip holds
-                 the calibration probes) + the C ABI (hipcc); block.cpp links
+  libws.so       the product: HIP kernels for gfx950 (kernels.hip; quant.hip: 8-bit
+                 pools and token windows; peaks.hip holds the calibration
+                 probes) + the C ABI (hipcc); block.cpp links
                  hipBLASLt for the projections around the attention
   libws_host.so  host-only page-table entry points for CPU tests (g++)
 """
@@ -18,7 +19,7 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB_PATH = os.path.join(PKG, "libws.so")
 HOST_LIB_PATH = os.path.join(PKG, "libws_host.so")
 
-HIP_SOURCES = ["kernels.hip", "peaks.hip", "ws_api.cpp", "pagetable.cpp", "block.cpp"]
+HIP_SOURCES = ["kernels.hip", "quant.hip", "peaks.hip", "ws_api.cpp", "pagetable.cpp", "block.cpp"]
 # hipBLASLt runs the two projections of ws_block_step (plain GEMMs)
 LINK_FLAGS = ["-L/opt/rocm/lib", "-Wl,-rpath,/opt/rocm/lib", "-lhipblaslt"]
 # Packed fp32 ops are kept out of the generated code on purpose.  The kernels

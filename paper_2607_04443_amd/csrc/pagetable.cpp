@@ -128,4 +128,24 @@ void PageTable::visible_pages_append(const MaskSpec& mask, std::vector<PageRef>*
   }
 }
 
+int64_t PageTable::timeline_pages(const MaskSpec& mask, std::vector<PageRef>* out) const {
+  order_.clear();
+  for (const auto& s : segments_)
+    if (segment_visible(s, mask)) order_.push_back(&s);
+  std::sort(order_.begin(), order_.end(), [](const Segment* a, const Segment* b) {
+    return a->unit != b->unit ? a->unit < b->unit : a->kind < b->kind;
+  });
+  int64_t n_tokens = 0;
+  for (const Segment* s : order_) {
+    int32_t left = s->n_tokens;
+    for (int32_t p : s->pages) {
+      const int32_t n = std::min(left, page_tokens_);
+      out->push_back(PageRef{p, n});
+      left -= n;
+    }
+    n_tokens += s->n_tokens;
+  }
+  return n_tokens;
+}
+
 }  // namespace ws

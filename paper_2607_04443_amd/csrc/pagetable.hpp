@@ -64,6 +64,9 @@ class PageTable {
   // The same list, appended to *out (for the concatenated lists of a call
   // whose queries belong to several units).
   void visible_pages_append(const MaskSpec& mask, std::vector<PageRef>* out) const;
+  // The visible pages ordered by unit, then kind, then token (appended to *out):
+  // the timeline of a token window; returns its token count.
+  int64_t timeline_pages(const MaskSpec& mask, std::vector<PageRef>* out) const;
   static bool segment_visible(const Segment& s, const MaskSpec& mask);
 
  private:
@@ -76,6 +79,7 @@ class PageTable {
   std::vector<Segment> segments_;
   uint64_t serial_ = 0;
   uint64_t version_ = 1;
+  mutable std::vector<const Segment*> order_;  // timeline_pages' own
 };
 
 }  // namespace ws

@@ -57,6 +57,18 @@ WSH_API int32_t wsh_visible(void* pt, int32_t q_unit, int32_t min_unit, uint32_t
   return static_cast<int32_t>(out.size());
 }
 
+// The same in the order of a token window's timeline; *n_tokens: its tokens.
+WSH_API int32_t wsh_timeline(void* pt, int32_t q_unit, int32_t min_unit, uint32_t kind_mask, int32_t* pages,
+                             int32_t* n_valid, int32_t cap, int64_t* n_tokens) {
+  std::vector<ws::PageRef> out;
+  *n_tokens = static_cast<ws::PageTable*>(pt)->timeline_pages(ws::MaskSpec{q_unit, min_unit, kind_mask}, &out);
+  for (int32_t i = 0; i < cap && i < static_cast<int32_t>(out.size()); ++i) {
+    pages[i] = out[static_cast<size_t>(i)].page;
+    n_valid[i] = out[static_cast<size_t>(i)].n_valid;
+  }
+  return static_cast<int32_t>(out.size());
+}
+
 // Page ids of one segment; returns the count, or -1 if absent.
 WSH_API int32_t wsh_segment_pages(void* pt, int32_t unit, int32_t kind, int32_t* pages, int32_t cap) {
   const ws::Segment* s = static_cast<const ws::PageTable*>(pt)->find(unit, kind);

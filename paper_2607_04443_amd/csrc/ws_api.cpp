@@ -99,11 +99,14 @@ struct QueryGroup {
 
 // A page list uploaded to the device arena: the concatenated visible lists
 // of a call's query groups (one per group with rows), kept while the cache
-// structure does not change.
+// structure does not change.  A token window's list also depends on the window
+// and the rows (`window`; off for other calls).
 struct ListCacheEntry {
   bool valid = false;
   int32_t n_masks = 0;
   ws::MaskSpec masks[ws::kMaxClasses]{};
+  ws::TokenWindow window{};
+  int32_t window_rows = 0;
   uint64_t version = 0;
   size_t offset = 0;
   int32_t n = 0;
@@ -113,10 +116,16 @@ bool same_mask(const ws::MaskSpec& a, const ws::MaskSpec& b) {
   return a.q_unit == b.q_unit && a.min_visible_unit == b.min_visible_unit && a.kind_mask == b.kind_mask;
 }
 
+bool same_window(const ws::TokenWindow& a, const ws::TokenWindow& b) {
+  return a.on == b.on && a.causal == b.causal && a.t0 == b.t0 && a.window == b.window && a.sinks == b.sinks &&
+         a.n_keys == b.n_keys;
+}
+
 }  // namespace
 
 struct ws_cache {
   ws_cache_config cfg{};
+  ws_kv_format format = WS_KV_BF16;
   int device = 0;
   int num_cus = 256;
   ws::PageTable pt;
@@ -143,6 +152,8 @@ struct ws_cache {
   int32_t opt_class_cus = 0;  // 0: classes share one round of the CUs, 1: each sized for all CUs
   int32_t opt_separate_audio = 0;  // 1: ws_step_attention never lets audio rows ride in the video kernel
   float* knorm2 = nullptr;  // [max_pages][H] squared key-norm maxima
+  float* kscale = nullptr;  // 8-bit pools: [max_pages][H] scales
+  float* vscale = nullptr;
   uint16_t* zeros = nullptr;  // 1 KB of zeros (direct-load source of empty blocks)
   void* static_ws = nullptr;  // device address of the static split-KV workspace on this device
   std::vector<ws::PageRef> scratch_list;
@@ -270,12 +281,13 @@ ws_status upload_list(ws_cache* c, const std::vector<ws::PageRef>& list, hipStre
 
 // The concatenated visible page lists of masks[0..n_masks) (c->scratch_list
 // holds them, built by the caller) in the device arena: reused while the
-// cache structure and the masks are unchanged, else uploaded once.
-ws_status arena_list(ws_cache* c, const ws::MaskSpec* masks, int n_masks, hipStream_t stream,
-                     const int2** dev) {
+// cache structure, the masks and the token window are unchanged, else uploaded once.
+ws_status arena_list(ws_cache* c, const ws::MaskSpec* masks, int n_masks, const ws::TokenWindow& window,
+                     int32_t window_rows, hipStream_t stream, const int2** dev) {
   const uint64_t ver = c->pt.version();
   for (auto& e : c->lists) {
     if (!e.valid || e.version != ver || e.n_masks != n_masks) continue;
+    if (!same_window(e.window, window) || e.window_rows != window_rows) continue;
     bool same = true;
     for (int i = 0; i < n_masks && same; ++i) same = same_mask(e.masks[i], masks[i]);
     if (same) {
@@ -291,6 +303,8 @@ ws_status arena_list(ws_cache* c, const ws::MaskSpec* masks, int n_masks, hipStr
   e.valid = true;
   e.n_masks = n_masks;
   for (int i = 0; i < n_masks; ++i) e.masks[i] = masks[i];
+  e.window = window;
+  e.window_rows = window_rows;
   e.version = ver;
   e.offset = off;
   e.n = static_cast<int32_t>(c->scratch_list.size());
@@ -344,7 +358,10 @@ void free_all(ws_cache* c) {
   if (c->apart_o) (void)hipFree(c->apart_o);
   if (c->apart_lse) (void)hipFree(c->apart_lse);
   if (c->knorm2) (void)hipFree(c->knorm2);
+  if (c->kscale) (void)hipFree(c->kscale);
+  if (c->vscale) (void)hipFree(c->vscale);
   if (c->zeros) (void)hipFree(c->zeros);
+  c->kscale = c->vscale = nullptr;
   c->knorm2 = nullptr;
   c->zeros = nullptr;
   c->kpool = c->vpool = nullptr;
@@ -354,9 +371,11 @@ void free_all(ws_cache* c) {
   c->part_o = c->part_lse = c->apart_o = c->apart_lse = nullptr;
 }
 
-ws_status create_impl(const ws_cache_config* cfg, ws_cache** out) {
+ws_status create_impl(const ws_cache_config* cfg, ws_kv_format format, ws_cache** out) {
   if (!cfg || !out) return fail(WS_ERR_INVALID_ARG, "NULL argument");
   *out = nullptr;
+  if (format != WS_KV_BF16 && format != WS_KV_INT8 && format != WS_KV_E4M3)
+    return fail(WS_ERR_INVALID_ARG, "bad cache format %d", static_cast<int>(format));
   if (cfg->head_dim != ws::kHeadDim)
     return fail(WS_ERR_UNSUPPORTED, "head_dim %d unsupported (only 128)", cfg->head_dim);
   if (cfg->page_tokens != ws::kPageTokens)
@@ -379,6 +398,7 @@ ws_status create_impl(const ws_cache_config* cfg, ws_cache** out) {
 
   ws_cache* c = new ws_cache(cfg->page_tokens, cfg->max_pages);
   c->cfg = *cfg;
+  c->format = format;
   auto bail = [&](ws_status st) {
     free_all(c);
     delete c;
@@ -389,13 +409,20 @@ ws_status create_impl(const ws_cache_config* cfg, ws_cache** out) {
   e = hipDeviceGetAttribute(&c->num_cus, hipDeviceAttributeMultiprocessorCount, c->device);
   if (e != hipSuccess) return bail(hip_fail(e, "hipDeviceGetAttribute"));
 
-  const size_t pool_elems =
-      static_cast<size_t>(cfg->max_pages) * cfg->num_heads * static_cast<size_t>(ws::kPageHeadElems);
-  if ((e = hipMalloc(&c->kpool, pool_elems * 2)) != hipSuccess) return bail(hip_fail(e, "hipMalloc(K pool)"));
-  if ((e = hipMalloc(&c->vpool, pool_elems * 2)) != hipSuccess) return bail(hip_fail(e, "hipMalloc(V pool)"));
-  if ((e = hipMemset(c->kpool, 0, pool_elems * 2)) != hipSuccess) return bail(hip_fail(e, "hipMemset"));
-  if ((e = hipMemset(c->vpool, 0, pool_elems * 2)) != hipSuccess) return bail(hip_fail(e, "hipMemset"));
+  const size_t pool_bytes = static_cast<size_t>(cfg->max_pages) * cfg->num_heads *
+                            static_cast<size_t>(ws::kPageHeadElems) * (format == WS_KV_BF16 ? 2 : 1);
+  if ((e = hipMalloc(&c->kpool, pool_bytes)) != hipSuccess) return bail(hip_fail(e, "hipMalloc(K pool)"));
+  if ((e = hipMalloc(&c->vpool, pool_bytes)) != hipSuccess) return bail(hip_fail(e, "hipMalloc(V pool)"));
+  if ((e = hipMemset(c->kpool, 0, pool_bytes)) != hipSuccess) return bail(hip_fail(e, "hipMemset"));
+  if ((e = hipMemset(c->vpool, 0, pool_bytes)) != hipSuccess) return bail(hip_fail(e, "hipMemset"));
   const size_t norm_elems = static_cast<size_t>(cfg->max_pages) * cfg->num_heads;
+  if (format != WS_KV_BF16) {
+    for (float** scales : {&c->kscale, &c->vscale}) {
+      if ((e = hipMalloc(scales, norm_elems * sizeof(float))) != hipSuccess)
+        return bail(hip_fail(e, "hipMalloc(scales)"));
+      if ((e = hipMemset(*scales, 0, norm_elems * sizeof(float))) != hipSuccess) return bail(hip_fail(e, "hipMemset"));
+    }
+  }
   if ((e = hipMalloc(&c->knorm2, norm_elems * sizeof(float))) != hipSuccess)
     return bail(hip_fail(e, "hipMalloc(key norms)"));
   if ((e = hipMemset(c->knorm2, 0, norm_elems * sizeof(float))) != hipSuccess)
@@ -461,6 +488,7 @@ float scale_log2_of(float softmax_scale) {
 // One attention call, validated and resolved into launch arguments.
 struct AttnPlan {
   bool audio = false;
+  bool few = false;  // the kernel of 8-bit pages and token windows (quant.hip)
   ws::AttnArgs a{};
   bool merge = false;
   ws::CombineArgs cb{};
@@ -468,10 +496,55 @@ struct AttnPlan {
   int64_t part_rows = 0;  // (range, head, query) partial rows the kernel may write
 };
 
+// A page list that does not fit the kernel arguments goes through the arena, whose
+// contents a replayed graph would find replaced.
+ws_status refuse_capture(hipStream_t stream) {
+  hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
+  WS_HIP(hipStreamIsCapturing(stream, &cs));
+  if (cs != hipStreamCaptureStatusNone)
+    return fail(WS_ERR_UNSUPPORTED, "a call with more than %d visible pages cannot be captured",
+                ws::AttnArgs::kInlinePages);
+  return WS_OK;
+}
+
+constexpr int32_t kMaxTimeline = 1 << 24;  // tokens a window's page entries can index
+constexpr int32_t kMaxWindow = 1 << 30;
+
+// The pages of a token window's timeline that some of its n_q rows see, into
+// c->scratch_list (entry: valid | first index << 7), and the kernel's window.
+ws_status window_pages(ws_cache* c, const ws_window_spec& w, int32_t n_q, ws::TokenWindow* out) {
+  std::vector<ws::PageRef>& list = c->scratch_list;
+  list.clear();
+  const int64_t n = c->pt.timeline_pages(
+      ws::MaskSpec{w.mask.q_unit, w.mask.min_visible_unit, w.mask.kind_mask}, &list);
+  if (n > kMaxTimeline)
+    return fail(WS_ERR_SHAPE, "timeline of %lld tokens (at most 2^24)", static_cast<long long>(n));
+  ws::TokenWindow t{};
+  t.on = 1;
+  t.causal = w.causal;
+  t.n_keys = static_cast<int32_t>(n);
+  t.t0 = w.q_start == WS_WINDOW_AT_END ? t.n_keys - n_q : w.q_start;
+  t.window = w.window == 0 ? kMaxWindow : std::min(w.window, kMaxWindow);
+  t.sinks = std::min(w.n_sink, t.n_keys);
+  // seen by some row: [lo of the first row, hi of the last), and the sinks below
+  const int32_t hi = w.causal ? std::min(t.t0 + n_q, t.n_keys) : t.n_keys;
+  const int32_t lo = t.t0 + 1 - t.window;
+  size_t kept = 0;
+  int32_t start = 0;
+  for (const ws::PageRef p : list) {  // (a copy: the list is rewritten in place)
+    if (start < hi && (start + p.n_valid > lo || start < t.sinks))
+      list[kept++] = ws::PageRef{p.page, p.n_valid | static_cast<int32_t>(static_cast<uint32_t>(start) << 7)};
+    start += p.n_valid;
+  }
+  list.resize(kept);
+  *out = t;
+  return WS_OK;
+}
+
 ws_status plan_attention(bool audio, const void* q, int64_t q_tok_stride, int64_t q_head_stride,
                          int32_t n_groups, const QueryGroup* groups, const ws_query_desc* qd, ws_cache* c,
                          void* out, int64_t out_tok_stride, int64_t out_head_stride,
-                         hipStream_t stream, AttnPlan* plan) {
+                         hipStream_t stream, AttnPlan* plan, const ws_window_spec* window = nullptr) {
   if (!c || !qd || !groups) return fail(WS_ERR_INVALID_ARG, "NULL argument");
   if (ws_status st = check_device(c); st != WS_OK) return st;
   if (n_groups < 1 || n_groups > (audio ? 1 : ws::kMaxClasses))
@@ -497,11 +570,21 @@ ws_status plan_attention(bool audio, const void* q, int64_t q_tok_stride, int64_
   if (!std::isfinite(qd->softmax_scale) || qd->softmax_scale < 0.f)
     return fail(WS_ERR_INVALID_ARG, "bad softmax_scale");
 
+  if (window) {
+    if (window->window < 0 || window->n_sink < 0)
+      return fail(WS_ERR_INVALID_ARG, "window %d and n_sink %d must be >= 0", window->window, window->n_sink);
+    if (window->causal != 0 && window->causal != 1) return fail(WS_ERR_INVALID_ARG, "causal must be 0 or 1");
+    if (window->q_start < WS_WINDOW_AT_END || window->q_start > kMaxTimeline)
+      return fail(WS_ERR_INVALID_ARG, "q_start %d outside [0, 2^24] and not WS_WINDOW_AT_END", window->q_start);
+  }
+
   // Each group with rows is a query class with its own visible page list;
   // the lists are concatenated.  The whole list goes into the kernel
   // arguments when it fits, else into the device arena (one upload per
   // distinct list).
   plan->audio = audio;
+  plan->few = window || c->format != WS_KV_BF16;
+  const bool few_rows = audio || plan->few;  // key ranges of 16-row tiles, merged in fp32
   ws::AttnArgs& a = plan->a;
   a = ws::AttnArgs{};
   const int2* plist = nullptr;
@@ -515,7 +598,11 @@ ws_status plan_attention(bool audio, const void* q, int64_t q_tok_stride, int64_
     cl.q0 = r0;
     cl.n_q = groups[g].n_q;
     cl.page0 = static_cast<int32_t>(c->scratch_list.size());
-    c->pt.visible_pages_append(groups[g].mask, &c->scratch_list);
+    if (window) {
+      if (ws_status st = window_pages(c, *window, groups[g].n_q, &a.win); st != WS_OK) return st;
+    } else {
+      c->pt.visible_pages_append(groups[g].mask, &c->scratch_list);
+    }
     cl.n_pages = static_cast<int32_t>(c->scratch_list.size()) - cl.page0;
   }
   const int32_t n_pages = static_cast<int32_t>(c->scratch_list.size());
@@ -523,8 +610,10 @@ ws_status plan_attention(bool audio, const void* q, int64_t q_tok_stride, int64_
     for (int32_t i = 0; i < n_pages; ++i)
       a.inline_pages[i] = make_int2(c->scratch_list[static_cast<size_t>(i)].page,
                                     c->scratch_list[static_cast<size_t>(i)].n_valid);
-  } else if (ws_status st = arena_list(c, masks, n_cls, stream, &plist); st != WS_OK) {
-    return st;
+  } else {
+    if (plan->few)
+      if (ws_status st = refuse_capture(stream); st != WS_OK) return st;
+    if (ws_status st = arena_list(c, masks, n_cls, a.win, window ? n_q : 0, stream, &plist); st != WS_OK) return st;
   }
   a.n_classes = n_cls;
   a.q = static_cast<const uint16_t*>(q);
@@ -551,13 +640,16 @@ ws_status plan_attention(bool audio, const void* q, int64_t q_tok_stride, int64_
   a.part_o = audio ? c->apart_o : c->part_o;
   a.part_lse = audio ? c->apart_lse : c->part_lse;
   a.flags = c->flags_dev;
-  const int qtile = audio ? ws::kAudioQTile : ws::kVideoQTile;
+  a.format = static_cast<int32_t>(c->format);
+  a.kscale = c->kscale;
+  a.vscale = c->vscale;
+  const int qtile = few_rows ? ws::kAudioQTile : ws::kVideoQTile;
   a.n_qtiles = (n_q + qtile - 1) / qtile;
   const int n_items = a.n_qtiles * H;
   const int64_t cap = c->part_rows / (static_cast<int64_t>(H) * n_q);
   int splits = 1;         // audio: key ranges; video: workgroup groups
-  bool merge = audio;
-  if (audio) {
+  bool merge = few_rows;
+  if (few_rows) {
     splits = choose_audio_splits(c, n_items, n_pages);
     splits = std::max(1, std::min(splits, std::max(1, n_pages)));
     splits = static_cast<int>(std::min<int64_t>(splits, std::max<int64_t>(cap, 1)));
@@ -565,7 +657,7 @@ ws_status plan_attention(bool audio, const void* q, int64_t q_tok_stride, int64_
     splits = pps > 0 ? (n_pages + pps - 1) / pps : 1;  // no empty splits
     if (cap < splits) return fail(WS_ERR_SHAPE, "split-KV workspace too small");
     plan->part_rows = static_cast<int64_t>(splits) * H * n_q;
-    if (splits == 1 || (c->opt_audio_splits == 0 && n_pages <= kAudioDirectPages)) {
+    if (splits <= 1 || (c->opt_audio_splits == 0 && n_pages <= kAudioDirectPages)) {
       splits = 1;
       a.audio_direct = 1;
       merge = false;
@@ -634,15 +726,15 @@ ws_status plan_attention(bool audio, const void* q, int64_t q_tok_stride, int64_
 
   plan->splits = splits;
   plan->merge = merge;
-  if (merge || audio) {  // (audio: also what a step's rider rows take over)
+  if (merge || few_rows) {  // (audio: also what a step's rider rows take over)
     ws::CombineArgs& cb = plan->cb;
     cb = ws::CombineArgs{};
     cb.part_o = a.part_o;
     cb.part_lse = a.part_lse;
-    cb.n_splits = audio ? splits : kMaxVideoSplits;
-    cb.n_groups = audio ? 0 : splits;
-    cb.n_classes = audio ? 0 : a.n_classes;
-    if (!audio)
+    cb.n_splits = few_rows ? splits : kMaxVideoSplits;
+    cb.n_groups = few_rows ? 0 : splits;
+    cb.n_classes = few_rows ? 0 : a.n_classes;
+    if (!few_rows)
       for (int k = 0; k < a.n_classes; ++k) cb.cls[k] = a.cls[k];
     cb.seg_cost = a.seg_cost;
     cb.n_q = n_q;
@@ -656,15 +748,27 @@ ws_status plan_attention(bool audio, const void* q, int64_t q_tok_stride, int64_
 
 hipError_t launch_plan_kernel(const AttnPlan& p, hipStream_t stream, hipEvent_t start = nullptr,
                               hipEvent_t stop = nullptr) {
-  return p.audio ? ws::launch_audio_attention(p.a, stream, start, stop)
-                 : ws::launch_unit_attention(p.a, stream, start, stop);
+  return p.few     ? ws::launch_few_attention(p.a, stream, start, stop)
+         : p.audio ? ws::launch_audio_attention(p.a, stream, start, stop)
+                   : ws::launch_unit_attention(p.a, stream, start, stop);
 }
-
 
 // A timed attention call: events 0 and 1 are the kernel's own dispatch
 // timestamps (see launch_plan_kernel), event 2 follows the merge.
 ws_status timing_begin(ws_cache* c, const AttnPlan& p, hipStream_t stream, int* slot) {
-  return timing_begin_path(c, p.audio ? 1 : 0, p.splits, stream, slot, true);
+  return timing_begin_path(c, p.a.win.on ? 6 : p.audio ? 1 : 0, p.splits, stream, slot, true);
+}
+
+ws_status run_plan(ws_cache* c, const AttnPlan& p, hipStream_t stream) {
+  int slot = -1;
+  if (ws_status st = timing_begin(c, p, stream, &slot); st != WS_OK) return st;
+  hipError_t e = launch_plan_kernel(p, stream, timing_event(c, slot, 0), timing_event(c, slot, 1));
+  if (e != hipSuccess) return hip_fail(e, p.audio ? "audio_attn launch" : "unit_attn launch");
+  if (p.merge) {
+    e = ws::launch_combine(p.cb, stream);
+    if (e != hipSuccess) return hip_fail(e, "combine launch");
+  }
+  return timing_mark(c, slot, 2, stream);
 }
 
 
@@ -674,19 +778,37 @@ ws_status attention_impl(bool audio, const void* q, int64_t q_tok_stride, int64_
                          void* hip_stream) {
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   AttnPlan p;
+  if (c && c->format != WS_KV_BF16 && groups && qd && n_groups > 1) {  // 8-bit pages: one call per group
+    int32_t n_q = 0, last = 0;
+    for (int g = 0; g < n_groups; ++g) {
+      if (groups[g].n_q < 0) return fail(WS_ERR_SHAPE, "query group %d has a negative row count", g);
+      n_q += groups[g].n_q;
+      if (groups[g].n_q > 0) last = g;
+    }
+    if (n_q < 1 || n_q > c->cfg.max_q_tokens)
+      return fail(WS_ERR_SHAPE, "n_q %d out of range [1, %d]", n_q, c->cfg.max_q_tokens);
+    if (ws_status st = check_strides("q", q, q_tok_stride, q_head_stride, n_q, c->cfg.num_heads); st != WS_OK) return st;
+    if (ws_status st = check_strides("out", out, out_tok_stride, out_head_stride, n_q, c->cfg.num_heads); st != WS_OK)
+      return st;
+    int64_t r0 = 0;
+    for (int g = 0; g <= last; r0 += groups[g].n_q, ++g) {
+      if (groups[g].n_q == 0) continue;
+      ws_query_desc d = *qd;
+      if (d.positions) d.positions += 3 * r0;
+      if (ws_status st = attention_impl(audio, static_cast<const uint16_t*>(q) + r0 * q_tok_stride, q_tok_stride,
+                                        q_head_stride, 1, groups + g, &d, c,
+                                        static_cast<uint16_t*>(out) + r0 * out_tok_stride, out_tok_stride,
+                                        out_head_stride, hip_stream);
+          st != WS_OK)
+        return st;
+    }
+    return WS_OK;
+  }
   if (ws_status st = plan_attention(audio, q, q_tok_stride, q_head_stride, n_groups, groups, qd, c, out,
                                     out_tok_stride, out_head_stride, stream, &p);
       st != WS_OK)
     return st;
-  int slot = -1;
-  if (ws_status st = timing_begin(c, p, stream, &slot); st != WS_OK) return st;
-  hipError_t e = launch_plan_kernel(p, stream, timing_event(c, slot, 0), timing_event(c, slot, 1));
-  if (e != hipSuccess) return hip_fail(e, audio ? "audio_attn launch" : "unit_attn launch");
-  if (p.merge) {
-    e = ws::launch_combine(p.cb, stream);
-    if (e != hipSuccess) return hip_fail(e, "combine launch");
-  }
-  return timing_mark(c, slot, 2, stream);
+  return run_plan(c, p, stream);
 }
 
 // Audio partial rows (fp32 O and log-sum-exp) the static workspace holds next to
@@ -711,7 +833,7 @@ ws_status use_static_workspace(ws_cache* c, AttnPlan& pv, AttnPlan& pa) {
     return p;
   };
   const size_t rv = static_cast<size_t>(pv.part_rows), ra = static_cast<size_t>(pa.part_rows);
-  float* vo = reinterpret_cast<float*>(take(rv * ws::kHeadDim * sizeof(uint16_t)));
+  float* vo = reinterpret_cast<float*>(take(rv * ws::kHeadDim * (pv.few ? sizeof(float) : sizeof(uint16_t))));
   float* vl = reinterpret_cast<float*>(take(rv * sizeof(float)));
   float* ao = reinterpret_cast<float*>(take(ra * ws::kHeadDim * sizeof(float)));
   float* al = reinterpret_cast<float*>(take(ra * sizeof(float)));
@@ -746,7 +868,7 @@ ws_status use_static_workspace(ws_cache* c, AttnPlan& pv, AttnPlan& pa) {
 // does not qualify.
 bool plan_riders(ws_cache* c, const ws_attn_call* video, const ws_attn_call* audio, AttnPlan& pv, AttnPlan& pa,
                  int64_t static_rows) {
-  if (c->opt_separate_audio || audio->desc.mode != WS_QUERY_PREPARED) return false;
+  if (c->format != WS_KV_BF16 || c->opt_separate_audio || audio->desc.mode != WS_QUERY_PREPARED) return false;
   if (pv.a.n_classes != 1 || pv.a.cls[0].n_pages == 0) return false;
   const ws::AttnClass& cl = pv.a.cls[0];
   const int H = c->cfg.num_heads;
@@ -908,7 +1030,11 @@ ws_status step_attention_impl(ws_cache* c, const ws_attn_call* video, const ws_a
   } else if (ws_status st = timing_mark(c, sa, 1, stream); st != WS_OK) {
     return st;
   }
-  if (pv.merge || pa.merge) {
+  if (pv.few) {  // (8-bit pages: both calls' ranges are the audio merge's)
+    for (const AttnPlan* p : {&pv, &pa})
+      if (p->merge)
+        if (e = ws::launch_combine(p->cb, stream); e != hipSuccess) return hip_fail(e, "combine launch");
+  } else if (pv.merge || pa.merge) {
     ws::CombineArgs none{};
     e = ws::launch_step_combine(pv.merge ? pv.cb : none, pa.merge ? pa.cb : none, stream);
     if (e != hipSuccess) return hip_fail(e, "combine launch");
@@ -916,16 +1042,87 @@ ws_status step_attention_impl(ws_cache* c, const ws_attn_call* video, const ws_a
   return timing_mark(c, sa, 2, stream);
 }
 
+// What an 8-bit code stands for, and a float rounded to bf16 (finite values).
+float code_value(ws_kv_format format, uint8_t code) {
+  if (format == WS_KV_INT8) return static_cast<float>(static_cast<int8_t>(code));
+  const int e = (code >> 3) & 15, f = code & 7;
+  const float v = e ? std::ldexp(static_cast<float>(8 + f), e - 10) : std::ldexp(static_cast<float>(f), -9);
+  return code & 0x80 ? -v : v;
+}
+uint16_t bf16_bits(float v) {
+  uint32_t u;
+  std::memcpy(&u, &v, 4);
+  return static_cast<uint16_t>((u + 0x7fffu + ((u >> 16) & 1u)) >> 16);
+}
+
+// A segment's codes in token order and its pages' scales (any may be NULL).
+ws_status export_codes(ws_cache* c, const ws::Segment& s, uint8_t* k, uint8_t* v, float* ks, float* vs) {
+  const size_t H = static_cast<size_t>(c->cfg.num_heads), page_bytes = H * ws::kPageHeadElems;
+  std::vector<uint8_t> tile(page_bytes);
+  for (size_t pi = 0; pi < s.pages.size(); ++pi) {
+    const size_t page = static_cast<size_t>(s.pages[pi]);
+    const int valid = std::min(s.n_tokens - static_cast<int32_t>(pi) * ws::kPageTokens, ws::kPageTokens);
+    for (int pool = 0; pool < 2; ++pool) {
+      uint8_t* const out = pool ? v : k;
+      if (float* scales = pool ? vs : ks)
+        WS_HIP(hipMemcpy(scales + pi * H, (pool ? c->vscale : c->kscale) + page * H, H * sizeof(float),
+                         hipMemcpyDeviceToHost));
+      if (!out) continue;
+      WS_HIP(hipMemcpy(tile.data(), reinterpret_cast<const uint8_t*>(pool ? c->vpool : c->kpool) + page * page_bytes,
+                       page_bytes, hipMemcpyDeviceToHost));
+      for (int slot = 0; slot < valid; ++slot)
+        for (size_t h = 0; h < H; ++h)
+          for (int d = 0; d < ws::kHeadDim; ++d)
+            out[((pi * ws::kPageTokens + static_cast<size_t>(slot)) * H + h) * ws::kHeadDim + static_cast<size_t>(d)] =
+                tile[h * ws::kPageHeadElems +
+                     static_cast<size_t>(pool ? ws::v8_tile_index(slot, d) : ws::k8_tile_index(slot, d))];
+    }
+  }
+  return WS_OK;
+}
+
+// The values they stand for, rounded to bf16 (either may be NULL).
+ws_status export_values(ws_cache* c, const ws::Segment& s, uint16_t* k, uint16_t* v) {
+  try {
+    const size_t H = static_cast<size_t>(c->cfg.num_heads), row = H * ws::kHeadDim;
+    const size_t n = static_cast<size_t>(s.n_tokens) * row;
+    std::vector<uint8_t> codes[2] = {std::vector<uint8_t>(n), std::vector<uint8_t>(n)};
+    std::vector<float> scales[2] = {std::vector<float>(s.pages.size() * H), std::vector<float>(s.pages.size() * H)};
+    if (ws_status st = export_codes(c, s, codes[0].data(), codes[1].data(), scales[0].data(), scales[1].data());
+        st != WS_OK)
+      return st;
+    for (int i = 0; i < 2; ++i) {
+      uint16_t* const out = i ? v : k;
+      for (size_t j = 0; out && j < n; ++j)
+        out[j] = bf16_bits(code_value(c->format, codes[i][j]) *
+                           scales[i][j / row / ws::kPageTokens * H + j % row / ws::kHeadDim]);
+    }
+    return WS_OK;
+  } catch (...) {
+    return fail(WS_ERR_INVALID_ARG, "host allocation failed");
+  }
+}
+
 }  // namespace
 
 extern "C" {
 
 ws_status ws_cache_create(const ws_cache_config* cfg, ws_cache** out) {
+  return ws_cache_create_format(cfg, WS_KV_BF16, out);
+}
+
+ws_status ws_cache_create_format(const ws_cache_config* cfg, ws_kv_format format, ws_cache** out) {
   try {
-    return create_impl(cfg, out);
+    return create_impl(cfg, format, out);
   } catch (...) {
     return fail(WS_ERR_INVALID_ARG, "host allocation failed");
   }
+}
+
+ws_status ws_cache_format(const ws_cache* c, ws_kv_format* format) {
+  if (!c || !format) return fail(WS_ERR_INVALID_ARG, "NULL argument");
+  *format = c->format;
+  return WS_OK;
 }
 
 ws_status ws_cache_destroy(ws_cache* cache) {
@@ -1054,6 +1251,9 @@ ws_status ws_step_append(ws_cache* c, int32_t n, const ws_append_item* items, in
   a.knorm2 = c->knorm2;
   a.rope = c->rope;
   a.flags = c->flags_dev;
+  a.format = static_cast<int32_t>(c->format);
+  a.kscale = c->kscale;
+  a.vscale = c->vscale;
   int n_segs = 0;
   int tslot = -1;
   if (ws_status st = timing_begin_path(c, 2, n + n_q, stream, &tslot, true); st != WS_OK) {
@@ -1067,7 +1267,8 @@ ws_status ws_step_append(ws_cache* c, int32_t n, const ws_append_item* items, in
     if (a.n_blocks == 0) return hipSuccess;
     hipEvent_t ev0 = started ? nullptr : timing_event(c, tslot, 0);
     hipEvent_t ev1 = final_launch ? timing_event(c, tslot, 1) : nullptr;
-    const hipError_t e = ws::launch_kv_append(a, stream, ev0, ev1);
+    const hipError_t e = c->format == WS_KV_BF16 ? ws::launch_kv_append(a, stream, ev0, ev1)
+                                                 : ws::launch_kv_append_q(a, stream, ev0, ev1);
     started = started || ev0 != nullptr;
     stopped = stopped || ev1 != nullptr;
     a.n_blocks = 0;
@@ -1165,6 +1366,69 @@ ws_status ws_step_append(ws_cache* c, int32_t n, const ws_append_item* items, in
   return timing_mark(c, tslot, 2, stream);
 }
 
+ws_status ws_kv_gather(ws_cache* c, int32_t n, const ws_gather_item* items, void* hip_stream) {
+  if (!c || !items) return fail(WS_ERR_INVALID_ARG, "NULL argument");
+  if (n < 1 || n > WS_MAX_APPEND_ITEMS)
+    return fail(WS_ERR_INVALID_ARG, "gather item count %d outside [1, %d]", n, WS_MAX_APPEND_ITEMS);
+  if (ws_status st = check_device(c); st != WS_OK) return st;
+  const int H = c->cfg.num_heads;
+  for (int i = 0; i < n; ++i) {
+    const ws_gather_item& it = items[i];
+    if (ws_status st = check_kind(it.kind); st != WS_OK) return st;
+    const ws::Segment* seg = c->pt.find(it.unit, it.kind);
+    if (!seg)
+      return fail(WS_ERR_UNKNOWN_UNIT, "item %d: no segment for unit %d kind %d", i, it.unit, static_cast<int>(it.kind));
+    if (!it.k_out && !it.v_out) return fail(WS_ERR_INVALID_ARG, "item %d: no output", i);
+    for (void* p : {it.k_out, it.v_out})
+      if (p)
+        if (ws_status st = check_strides(p == it.k_out ? "k_out" : "v_out", p, it.tok_stride, it.head_stride,
+                                         seg->n_tokens, H);
+            st != WS_OK)
+          return st;
+  }
+  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  ws::GatherArgs a{};
+  a.num_heads = H;
+  a.format = static_cast<int32_t>(c->format);
+  a.kpool = c->kpool;
+  a.vpool = c->vpool;
+  a.kscale = c->kscale;
+  a.vscale = c->vscale;
+  int tslot = -1;
+  if (ws_status st = timing_begin_path(c, 7, n, stream, &tslot); st != WS_OK) return st;
+  int n_segs = 0;
+  auto flush = [&]() {
+    if (a.n_blocks == 0) return hipSuccess;
+    const hipError_t e = ws::launch_kv_gather(a, stream, nullptr, nullptr);
+    a.n_blocks = 0;
+    n_segs = 0;
+    return e;
+  };
+  for (int i = 0; i < n; ++i) {
+    const ws_gather_item& it = items[i];
+    const ws::Segment* seg = c->pt.find(it.unit, it.kind);
+    int slot = -1;
+    for (size_t p = 0; p < seg->pages.size(); ++p) {
+      if (a.n_blocks == ws::GatherArgs::kMaxPages || (slot < 0 && n_segs == ws::GatherArgs::kMaxSegs)) {
+        if (hipError_t e = flush(); e != hipSuccess) return hip_fail(e, "kv_gather launch");
+        slot = -1;
+      }
+      if (slot < 0) {
+        slot = n_segs++;
+        a.seg[slot] = ws::GatherSeg{static_cast<uint16_t*>(it.k_out), static_cast<uint16_t*>(it.v_out), it.tok_stride,
+                                    it.head_stride, seg->n_tokens};
+      }
+      a.pages[a.n_blocks] = seg->pages[p];
+      a.blk_page[a.n_blocks] = static_cast<int32_t>(p);
+      a.blk_seg[a.n_blocks] = static_cast<uint8_t>(slot);
+      ++a.n_blocks;
+    }
+  }
+  if (hipError_t e = flush(); e != hipSuccess) return hip_fail(e, "kv_gather launch");
+  if (ws_status st = timing_mark(c, tslot, 1, stream); st != WS_OK) return st;
+  return timing_mark(c, tslot, 2, stream);
+}
+
 ws_status ws_unit_commit(ws_cache* c, int32_t unit) {
   if (!c) return fail(WS_ERR_INVALID_ARG, "NULL cache");
   c->pt.commit(unit);
@@ -1211,6 +1475,24 @@ ws_status ws_unit_attention_groups(const void* q, int64_t q_tok_stride, int64_t 
                         out_head_stride, hip_stream);
 }
 
+ws_status ws_window_attention(const void* q, int64_t q_tok_stride, int64_t q_head_stride, int32_t n_q,
+                              const ws_query_desc* qdesc, ws_cache* cache, const ws_window_spec* window, void* out,
+                              int64_t out_tok_stride, int64_t out_head_stride, void* hip_stream) {
+  if (!window) return fail(WS_ERR_INVALID_ARG, "NULL argument");
+  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  const QueryGroup g{ws::MaskSpec{window->mask.q_unit, window->mask.min_visible_unit, window->mask.kind_mask}, n_q};
+  try {
+    AttnPlan p;
+    if (ws_status st = plan_attention(false, q, q_tok_stride, q_head_stride, 1, &g, qdesc, cache, out, out_tok_stride,
+                                      out_head_stride, stream, &p, window);
+        st != WS_OK)
+      return st;
+    return run_plan(cache, p, stream);
+  } catch (...) {
+    return fail(WS_ERR_INVALID_ARG, "host allocation failed");
+  }
+}
+
 ws_status ws_audio_attention(const void* q, int64_t q_tok_stride, int64_t q_head_stride, int32_t n_q,
                              const ws_query_desc* qdesc, ws_cache* cache, const ws_mask_spec* mask,
                              void* out, int64_t out_tok_stride, int64_t out_head_stride,
@@ -1238,6 +1520,7 @@ ws_status ws_cache_export(ws_cache* c, int32_t unit, ws_kind kind, void* k_host,
   if (!s) return fail(WS_ERR_UNKNOWN_UNIT, "no segment for unit %d kind %d", unit, static_cast<int>(kind));
   WS_HIP(hipDeviceSynchronize());
   const int H = c->cfg.num_heads;
+  if (c->format != WS_KV_BF16) return export_values(c, *s, static_cast<uint16_t*>(k_host), static_cast<uint16_t*>(v_host));
   const size_t page_elems = static_cast<size_t>(H) * ws::kPageHeadElems;
   std::vector<uint16_t> kp(page_elems), vp(page_elems);
   uint16_t* ko = static_cast<uint16_t*>(k_host);
@@ -1259,6 +1542,22 @@ ws_status ws_cache_export(ws_cache* c, int32_t unit, ws_kind kind, void* k_host,
     }
   }
   return WS_OK;
+}
+
+ws_status ws_cache_export_codes(ws_cache* c, int32_t unit, ws_kind kind, uint8_t* k_codes, uint8_t* v_codes,
+                                float* k_scales, float* v_scales) {
+  if (!c) return fail(WS_ERR_INVALID_ARG, "NULL cache");
+  if (c->format == WS_KV_BF16) return fail(WS_ERR_UNSUPPORTED, "a bf16 cache holds no codes");
+  if (ws_status st = check_device(c); st != WS_OK) return st;
+  if (ws_status st = check_kind(kind); st != WS_OK) return st;
+  const ws::Segment* s = c->pt.find(unit, kind);
+  if (!s) return fail(WS_ERR_UNKNOWN_UNIT, "no segment for unit %d kind %d", unit, static_cast<int>(kind));
+  try {
+    WS_HIP(hipDeviceSynchronize());
+    return export_codes(c, *s, k_codes, v_codes, k_scales, v_scales);
+  } catch (...) {
+    return fail(WS_ERR_INVALID_ARG, "host allocation failed");
+  }
 }
 
 ws_status ws_segment_tokens(ws_cache* c, int32_t unit, ws_kind kind, int32_t* n_tokens) {

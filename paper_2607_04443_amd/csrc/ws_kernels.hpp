@@ -32,8 +32,29 @@ __host__ __device__ constexpr int v_tile_index(int slot, int d) {
   return ((slot >> 5) * kHeadDim + d) * 32 + (slot & 31);
 }
 
+// Formats of a cache's pools.  In 8 bits a (page, head) tile is 8 KB of codes in
+// each pool, and value = code * scale with one fp32 scale per tile and pool:
+//   K pool: tile = [2 d halves][64 slots][64 d]
+//   V pool: tile = [128 d][64 slots]
+// so that one 16-byte load is 16 dims of a key, or 16 keys of a dim, and the 16
+// keys (or dims) of an MFMA operand tile cover whole 128-byte lines.
+//   int8: two's complement codes, scale = largest magnitude / 127 in fp32, rounded
+//         up to 16 significant bits: code * scale is exact in fp32, and no code
+//         exceeds 127.
+//   e4m3: scale = the least power of two >= 2^-126 that brings the largest
+//         magnitude to at most 448: a power of two costs a floating-point code
+//         nothing, and code * scale is exact in bf16.
+// The attention takes code * scale rounded to bf16, the type of its matrix
+// operands (and of a bf16 cache's keys).  Empty slots hold code 0.
+enum KvFormat : int32_t { kFmtBf16 = 0, kFmtInt8 = 1, kFmtE4m3 = 2 };
+__host__ __device__ constexpr int k8_tile_index(int slot, int d) {
+  return ((d >> 6) * kPageTokens + slot) * 64 + (d & 63);
+}
+__host__ __device__ constexpr int v8_tile_index(int slot, int d) { return d * kPageTokens + slot; }
+
 // Device error flags (ws_cache_check).
 constexpr uint32_t kFlagPositionClamped = 1u;
+constexpr uint32_t kFlagNotStored = 2u;  // an 8-bit append met an infinity, a NaN or a value too large (stored as 0)
 
 // Video work partition.  For one query tile the (head, page) units are laid
 // on a line in head-major order with seg_cost extra places in front of
@@ -193,9 +214,51 @@ struct AppendArgs {
   float* knorm2;
   RopeTables rope;
   uint32_t* flags;
+  int32_t format;        // KvFormat; 8-bit pools also take their scales
+  float* kscale;         // [page][head]
+  float* vscale;
   int32_t pages[kMaxAppendPages];
   int32_t blk_page[kMaxAppendPages];
   uint8_t blk_seg[kMaxAppendPages];
+};
+
+// One segment of a gather launch: codes and scales (or bf16 tiles) of its pages
+// back to bf16 rows.  Block x reads page pages[x], page blk_page[x] of segment
+// blk_seg[x].
+struct GatherSeg {
+  uint16_t* k;
+  uint16_t* v;
+  int64_t tok_stride;
+  int64_t head_stride;
+  int32_t n_tokens;
+};
+struct GatherArgs {
+  static constexpr int kMaxSegs = 8;
+  static constexpr int kMaxPages = 192;
+  GatherSeg seg[kMaxSegs];
+  int32_t n_blocks;
+  int32_t num_heads;
+  int32_t format;
+  const uint16_t* kpool;
+  const uint16_t* vpool;
+  const float* kscale;
+  const float* vscale;
+  int32_t pages[kMaxPages];
+  int32_t blk_page[kMaxPages];
+  uint8_t blk_seg[kMaxPages];
+};
+
+// Token window of an attention call.  The visible tokens under the call's mask,
+// in order, are the timeline; row i of the call sits at index t = t0 + i and sees
+// the keys j with (j > t - window or j < sinks), and j <= t when causal.  The
+// page list then carries each page's first index: entry y = valid | start << 7.
+struct TokenWindow {
+  int32_t on;       // 0: every key of the page list is visible to every row
+  int32_t causal;
+  int32_t t0;
+  int32_t window;   // 1 .. 2^30
+  int32_t sinks;
+  int32_t n_keys;   // tokens of the timeline
 };
 
 // Query class of a video attention call: the rows of one unit's queries in a
@@ -270,6 +333,10 @@ struct AttnArgs {
   int32_t rx_pages;
   int32_t rx_ranges;
   uint32_t* flags;
+  int32_t format;        // KvFormat of the pools
+  const float* kscale;   // 8-bit pools: [page][head]
+  const float* vscale;
+  TokenWindow win;
   int2 inline_pages[kInlinePages];
 };
 
@@ -308,6 +375,11 @@ hipError_t launch_unit_attention(const AttnArgs& a, hipStream_t stream, hipEvent
 hipError_t launch_audio_attention(const AttnArgs& a, hipStream_t stream, hipEvent_t start = nullptr,
                                   hipEvent_t stop = nullptr);
 hipError_t launch_combine(const CombineArgs& a, hipStream_t stream);
+// 8-bit pools, and token windows over any format (quant.hip): 4 independent waves
+// per (head, 16-query tile, key range), as the audio path.
+hipError_t launch_kv_append_q(const AppendArgs& a, hipStream_t stream, hipEvent_t start, hipEvent_t stop);
+hipError_t launch_kv_gather(const GatherArgs& a, hipStream_t stream, hipEvent_t start, hipEvent_t stop);
+hipError_t launch_few_attention(const AttnArgs& a, hipStream_t stream, hipEvent_t start, hipEvent_t stop);
 // The merges of a video call (n_groups > 0) and an audio call (num_heads > 0)
 // in one launch; either may be absent (zero-initialised).
 hipError_t launch_step_combine(const CombineArgs& video, const CombineArgs& audio, hipStream_t stream);

@@ -41,6 +41,8 @@ WS_APPEND_RAW, WS_APPEND_NORM_ROPE, WS_QUERY_PREPARED = 0, 1, 2
 WS_OPT_VIDEO_KV_SPLITS, WS_OPT_AUDIO_KV_SPLITS, WS_OPT_VIDEO_RUNNING_MAX = 0, 1, 2
 WS_OPT_VIDEO_CLASS_CUS = 3
 WS_OPT_STEP_SEPARATE_AUDIO = 4
+WS_KV_BF16, WS_KV_INT8, WS_KV_E4M3 = 0, 1, 2
+WS_WINDOW_AT_END = -1
 INT32_MIN = -(2 ** 31)
 
 
@@ -90,6 +92,16 @@ class ws_mask_spec(ctypes.Structure):
                 ("kind_mask", ctypes.c_uint32)]
 
 
+class ws_window_spec(ctypes.Structure):
+    _fields_ = [("mask", ws_mask_spec), ("window", ctypes.c_int32), ("n_sink", ctypes.c_int32),
+                ("causal", ctypes.c_int32), ("q_start", ctypes.c_int32)]
+
+
+class ws_gather_item(ctypes.Structure):
+    _fields_ = [("unit", ctypes.c_int32), ("kind", ctypes.c_int32), ("k_out", ctypes.c_void_p),
+                ("v_out", ctypes.c_void_p), ("tok_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
 class ws_attn_call(ctypes.Structure):
     _fields_ = [("q", ctypes.c_void_p), ("q_tok_stride", ctypes.c_int64),
                 ("q_head_stride", ctypes.c_int64), ("n_q", ctypes.c_int32),
@@ -127,11 +139,14 @@ _vp, _i32, _i64, _u32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.
 _P = ctypes.POINTER
 _SIGS = {
     "ws_cache_create": [_P(ws_cache_config), _P(_vp)],
+    "ws_cache_create_format": [_P(ws_cache_config), ctypes.c_int, _P(_vp)],
+    "ws_cache_format": [_vp, _P(ctypes.c_int)],
     "ws_cache_destroy": [_vp],
     "ws_cache_reset": [_vp],
     "ws_kv_append": [_vp, _vp, _vp, _i64, _i64, _P(ws_append_desc), _vp],
     "ws_kv_append_many": [_vp, _i32, _P(ws_append_item), _vp],
     "ws_step_append": [_vp, _i32, _P(ws_append_item), _i32, _P(ws_query_item), _vp],
+    "ws_kv_gather": [_vp, _i32, _P(ws_gather_item), _vp],
     "ws_unit_commit": [_vp, _i32],
     "ws_kv_evict_before": [_vp, _i32],
     "ws_kv_release": [_vp, _i32, _i32],
@@ -141,9 +156,12 @@ _SIGS = {
                            _i64, _i64, _vp],
     "ws_unit_attention_groups": [_vp, _i64, _i64, _i32, _P(ws_query_group), _P(ws_query_desc), _vp,
                                  _vp, _i64, _i64, _vp],
+    "ws_window_attention": [_vp, _i64, _i64, _i32, _P(ws_query_desc), _vp, _P(ws_window_spec), _vp,
+                            _i64, _i64, _vp],
     "ws_step_attention": [_vp, _P(ws_attn_call), _P(ws_attn_call), _vp],
     "ws_step_attention_noalloc": [_vp, _P(ws_attn_call), _P(ws_attn_call), _vp],
     "ws_cache_export": [_vp, _i32, _i32, _vp, _vp],
+    "ws_cache_export_codes": [_vp, _i32, _i32, _vp, _vp, _vp, _vp],
     "ws_block_create": [_vp, _vp, _vp, _i32, _P(_vp)],
     "ws_block_destroy": [_vp],
     "ws_block_step": [_vp, _P(ws_block_step_args), _vp],
@@ -187,6 +205,18 @@ def ws_cache_create(cfg: ws_cache_config) -> int:
     return h.value
 
 
+def ws_cache_create_format(cfg: ws_cache_config, fmt) -> int:
+    h = _vp()
+    _check(_lib.ws_cache_create_format(ctypes.byref(cfg), fmt, ctypes.byref(h)), "ws_cache_create_format")
+    return h.value
+
+
+def ws_cache_format(cache) -> int:
+    f = ctypes.c_int()
+    _check(_lib.ws_cache_format(cache, ctypes.byref(f)), "ws_cache_format")
+    return f.value
+
+
 def ws_cache_destroy(cache):
     _check(_lib.ws_cache_destroy(cache), "ws_cache_destroy")
 
@@ -214,6 +244,12 @@ def ws_step_append(cache, items, queries, stream):
            "ws_step_append")
 
 
+def ws_kv_gather(cache, items, stream):
+    """items: a sequence of ws_gather_item."""
+    arr = (ws_gather_item * max(len(items), 1))(*items)
+    _check(_lib.ws_kv_gather(cache, len(items), arr, stream), "ws_kv_gather")
+
+
 def ws_unit_commit(cache, unit):
     _check(_lib.ws_unit_commit(cache, unit), "ws_unit_commit")
 
@@ -238,6 +274,13 @@ def ws_audio_attention(q, q_tok_stride, q_head_stride, n_q, qdesc, cache, mask, 
     _check(_lib.ws_audio_attention(q, q_tok_stride, q_head_stride, n_q, ctypes.byref(qdesc), cache,
                                    ctypes.byref(mask), out, out_tok_stride, out_head_stride,
                                    stream), "ws_audio_attention")
+
+
+def ws_window_attention(q, q_tok_stride, q_head_stride, n_q, qdesc, cache, window, out,
+                        out_tok_stride, out_head_stride, stream):
+    _check(_lib.ws_window_attention(q, q_tok_stride, q_head_stride, n_q, ctypes.byref(qdesc), cache,
+                                    ctypes.byref(window), out, out_tok_stride, out_head_stride,
+                                    stream), "ws_window_attention")
 
 
 def ws_unit_attention_groups(q, q_tok_stride, q_head_stride, groups, qdesc, cache, out,
@@ -275,6 +318,11 @@ def ws_block_step(block, args: ws_block_step_args, stream):
 
 def ws_cache_export(cache, unit, kind, k_host, v_host):
     _check(_lib.ws_cache_export(cache, unit, kind, k_host, v_host), "ws_cache_export")
+
+
+def ws_cache_export_codes(cache, unit, kind, k_codes, v_codes, k_scales, v_scales):
+    _check(_lib.ws_cache_export_codes(cache, unit, kind, k_codes, v_codes, k_scales, v_scales),
+           "ws_cache_export_codes")
 
 
 def ws_segment_tokens(cache, unit, kind) -> int:
@@ -355,9 +403,10 @@ def ws_last_error() -> str:
 _APPEND_ITEM = struct.Struct("@PPqq" "iiiiPPf4x")
 _QUERY_DESC = struct.Struct("@i4xPPff")
 _QUERY_ITEM = struct.Struct("@Pqqi4x" "i4xPPff" "Pqq")
+_GATHER_ITEM = struct.Struct("@iiPPqq")
 _ATTN_CALL = struct.Struct("@Pqqi4x" "i4xPPff" "12s4x" "Pqq")
 for _layout, _type in ((_APPEND_ITEM, ws_append_item), (_QUERY_DESC, ws_query_desc),
-                       (_QUERY_ITEM, ws_query_item), (_ATTN_CALL, ws_attn_call)):
+                       (_QUERY_ITEM, ws_query_item), (_GATHER_ITEM, ws_gather_item), (_ATTN_CALL, ws_attn_call)):
     assert _layout.size == ctypes.sizeof(_type), _type
 _BF16 = torch.bfloat16
 _current_device = torch.cuda.current_device
@@ -394,18 +443,24 @@ def _query_desc(mode, positions, gamma, eps, scale):
 
 
 class Cache:
-    """Owns one ws_cache; methods mirror ws_kv_append / ws_unit_attention / ..."""
+    """Owns one ws_cache; methods mirror ws_kv_append / ws_unit_attention / ...
+    kv_format: what the cache holds keys and values in, 'bf16', 'int8' or 'e4m3'."""
+
+    FORMATS = {"bf16": WS_KV_BF16, "int8": WS_KV_INT8, "e4m3": WS_KV_E4M3}
 
     def __init__(self, num_heads, max_pages, max_q_tokens=1024, rope_max_pos=(65536, 256, 256),
-                 rope_pairs=(22, 21, 21), rope_theta=10000.0):
+                 rope_pairs=(22, 21, 21), rope_theta=10000.0, kv_format="bf16"):
+        self.handle = None
+        if kv_format not in self.FORMATS:
+            raise ValueError(f"kv_format must be one of {sorted(self.FORMATS)}")
         cfg = ws_cache_config()
         cfg.num_heads, cfg.head_dim, cfg.page_tokens = num_heads, 128, 64
         cfg.max_pages, cfg.max_q_tokens = max_pages, max_q_tokens
         cfg.rope_max_pos[:] = list(rope_max_pos)
         cfg.rope_pairs[:] = list(rope_pairs)
         cfg.rope_theta = rope_theta
-        self.num_heads = num_heads
-        self.handle = ws_cache_create(cfg)
+        self.num_heads, self.kv_format = num_heads, kv_format
+        self.handle = ws_cache_create_format(cfg, self.FORMATS[kv_format])
 
     def close(self):
         if self.handle:
@@ -472,6 +527,22 @@ class Cache:
         _check(_lib.ws_step_append(self.handle, len(items), arr, len(queries), qarr, _stream_handle(stream)),
                "ws_step_append")
 
+    def gather(self, items, stream=None):
+        """Segments out of the cache: dicts with unit, kind and k_out and/or v_out,
+        bf16 [tokens, heads, 128] device tensors (of the same strides)."""
+        packed = []
+        for x in items:
+            unit, kind, k, v = x["unit"], x["kind"], x.get("k_out"), x.get("v_out")
+            outs = [(n, t) for n, t in (("k_out", k), ("v_out", v)) if t is not None]
+            n_tok = ws_segment_tokens(self.handle, unit, kind)
+            for name, t in outs:
+                if _rows(name, t) != outs[0][1].stride() or tuple(t.shape) != (n_tok, self.num_heads, 128):
+                    raise ValueError(f"{name} must be [{n_tok}, {self.num_heads}, 128], both of the same strides")
+            st = outs[0][1].stride() if outs else (0, 0)
+            packed.append(_GATHER_ITEM.pack(unit, kind, _ptr(k), _ptr(v), st[0], st[1]))
+        arr = (ws_gather_item * max(len(packed), 1)).from_buffer_copy(b"".join(packed) or bytes(_GATHER_ITEM.size))
+        _check(_lib.ws_kv_gather(self.handle, len(packed), arr, _stream_handle(stream)), "ws_kv_gather")
+
     def _attn(self, fn, q, out, mask, mode, positions, gamma, eps, scale, stream):
         qs, os_ = _rows("q", q), _rows("out", out)
         fn(q.data_ptr(), qs[0], qs[1], q.shape[0], _query_desc(mode, positions, gamma, eps, scale),
@@ -528,6 +599,12 @@ class Cache:
         return self._attn(ws_audio_attention, q, out, mask, mode, positions, gamma, eps, scale,
                           stream)
 
+    def window_attention(self, q, out, window, mode=WS_APPEND_NORM_ROPE, positions=None, gamma=None,
+                         eps=1e-6, scale=0.0, stream=None):
+        """window: a ws_window_spec (window_spec())."""
+        return self._attn(ws_window_attention, q, out, window, mode, positions, gamma, eps, scale,
+                          stream)
+
     def commit(self, unit):
         ws_unit_commit(self.handle, unit)
 
@@ -545,6 +622,17 @@ class Cache:
         v = np.empty_like(k)
         ws_cache_export(self.handle, unit, kind, k.ctypes.data, v.ctypes.data)
         return k, v
+
+    def export_codes(self, unit, kind):
+        """An 8-bit cache's own contents: (K codes, V codes) as numpy uint8
+        [n, H, 128] and (K scales, V scales) as float32 [blocks, H]."""
+        import numpy as np
+        n = ws_segment_tokens(self.handle, unit, kind)
+        codes = [np.empty((n, self.num_heads, 128), dtype=np.uint8) for _ in range(2)]
+        scales = [np.empty((-(-n // 64), self.num_heads), dtype=np.float32) for _ in range(2)]
+        ws_cache_export_codes(self.handle, unit, kind, codes[0].ctypes.data, codes[1].ctypes.data,
+                              scales[0].ctypes.data, scales[1].ctypes.data)
+        return (*codes, *scales)
 
     def pages(self, unit, kind):
         """Pool page ids of a segment, in token order."""
@@ -566,10 +654,11 @@ class Cache:
     def timing_read(self):
         """Per-call launch timing recorded since the last read, oldest first:
         dicts with path ('video', 'audio', 'append', 'qkv_gemm', 'out_gemm', or
-        'audio_riders': a step's audio call with its rows in the video kernel),
-        n_splits, attn_us, merge_us."""
+        'audio_riders': a step's audio call with its rows in the video kernel,
+        'window', 'gather'), n_splits, attn_us, merge_us."""
         out = ws_cache_timing_read(self.handle, getattr(self, "_timing_cap", 0))
-        names = {0: "video", 1: "audio", 2: "append", 3: "qkv_gemm", 4: "out_gemm", 5: "audio_riders"}
+        names = {0: "video", 1: "audio", 2: "append", 3: "qkv_gemm", 4: "out_gemm", 5: "audio_riders",
+                 6: "window", 7: "gather"}
         return [dict(path=names.get(t.path, str(t.path)), n_splits=t.n_splits, attn_us=t.attn_us,
                      merge_us=t.merge_us) for t in out]
 
@@ -617,3 +706,13 @@ def mask_spec(q_unit, min_visible_unit=INT32_MIN, kinds=(WS_KIND_COND, WS_KIND_V
     m.q_unit, m.min_visible_unit = q_unit, min_visible_unit
     m.kind_mask = sum(1 << k for k in kinds)
     return m
+
+
+def window_spec(q_unit, window, n_sink=0, causal=True, q_start=WS_WINDOW_AT_END, min_visible_unit=INT32_MIN,
+                kinds=(WS_KIND_COND, WS_KIND_VIDEO)):
+    """A token window over the timeline of the tokens that mask_spec(q_unit,
+    min_visible_unit, kinds) leaves visible; window = 0 takes every earlier token."""
+    w = ws_window_spec()
+    w.mask = mask_spec(q_unit, min_visible_unit, kinds)
+    w.window, w.n_sink, w.causal, w.q_start = window, n_sink, int(causal), q_start
+    return w
