@@ -19,7 +19,7 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB_PATH = os.path.join(PKG, "libws.so")
 HOST_LIB_PATH = os.path.join(PKG, "libws_host.so")
 
-HIP_SOURCES = ["kernels.hip", "quant.hip", "peaks.hip", "ws_api.cpp", "pagetable.cpp", "block.cpp"]
+HIP_SOURCES = ["kernels.hip", "quant.hip", "video_paths.hip", "peaks.hip", "ws_api.cpp", "pagetable.cpp", "block.cpp"]
 # hipBLASLt runs the two projections of ws_block_step (plain GEMMs)
 LINK_FLAGS = ["-L/opt/rocm/lib", "-Wl,-rpath,/opt/rocm/lib", "-lhipblaslt"]
 # Packed fp32 ops are kept out of the generated code on purpose.  The kernels
@@ -64,7 +64,7 @@ def build(verbose=False):
                 "-D__HIP_PLATFORM_AMD__", "-I", "/opt/rocm/include", "-I", CSRC, os.path.join(CSRC, "pagetable.cpp"),
                 os.path.join(CSRC, "pagetable_capi.cpp"), "-o", host_tmp]
     jobs.append(host_cmd)
-    with ThreadPoolExecutor(max_workers=4) as ex:
+    with ThreadPoolExecutor(max_workers=6) as ex:
         list(ex.map(lambda c: _run(c, verbose), jobs))
     tmp = LIB_PATH + ".tmp"
     _run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp] + objs + LINK_FLAGS, verbose)

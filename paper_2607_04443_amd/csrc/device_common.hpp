@@ -113,6 +113,10 @@ __device__ __forceinline__ void load_pos(const RopeTables& r, const int32_t* pos
   clamp_pos(r, positions[3 * tok + 0], positions[3 * tok + 1], positions[3 * tok + 2], flags, pt, ph, pw);
 }
 
+// Read-only for a whole launch: accessed through the constant address space
+// so that uniform reads become scalar loads.
+typedef const __attribute__((address_space(4))) int2* const_page_list;
+
 typedef const __attribute__((address_space(4))) AppendSeg* const_append_seg;
 typedef const __attribute__((address_space(4))) AppendArgs* const_append_args;
 

@@ -302,9 +302,8 @@ __global__ __launch_bounds__(256, 2) void audio_attn_kernel(const AttnArgs a) {
   if (tid < 16) a.part_lse[row] = l_tot > 0.f ? big + __log2f(l_tot) : kNegInf;
 }
 
-#define WS_ONE_WAVE_PER_SIMD __launch_bounds__(kVideoWaves * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
-__global__ WS_ONE_WAVE_PER_SIMD void unit_attn_kernel(const AttnArgs a) { unit_attn<true>(a); }
-__global__ WS_ONE_WAVE_PER_SIMD void unit_attn_rows_kernel(const AttnArgs a) { unit_attn<false>(a); }
+__global__ WS_ONE_WAVE_PER_SIMD void unit_attn_kernel(const AttnArgs a) { unit_attn<PlainPath, kQueriesPrepared>(a); }
+__global__ WS_ONE_WAVE_PER_SIMD void unit_attn_rows_kernel(const AttnArgs a) { unit_attn<PlainPath, kQueriesRaw>(a); }
 
 // ------------------------------------------------------------------------- //
 // combine (audio key ranges): 16 threads per (head, query) row, 8 d each, 16

@@ -148,4 +148,44 @@ int64_t PageTable::timeline_pages(const MaskSpec& mask, std::vector<PageRef>* ou
   return n_tokens;
 }
 
+int64_t PageTable::timeline_tokens(const MaskSpec& mask) const {
+  int64_t n = 0;
+  for (const auto& s : segments_)
+    if (segment_visible(s, mask)) n += s.n_tokens;
+  return n;
+}
+
+void PageTable::window_pages(const MaskSpec& mask, const TokenWindow& w, int32_t n_q, std::vector<PageRef>* out) const {
+  const size_t first = out->size();
+  timeline_pages(mask, out);
+  // seen by some row: keys from the first row's lo to the last one's hi, and the sinks
+  const int32_t hi = std::min(w.t0 + n_q - 1 + w.ahead, w.n_keys), lo = w.t0 + 1 - w.window;
+  size_t kept = first;
+  int32_t start = 0;
+  for (size_t i = first; i < out->size(); ++i) {
+    const PageRef p = (*out)[i];  // (a copy: the list is rewritten in place)
+    if (start < hi && (start + p.n_valid > lo || start < w.sinks))
+      (*out)[kept++] = PageRef{p.page, p.n_valid | static_cast<int32_t>(static_cast<uint32_t>(start) << 7)};
+    start += p.n_valid;
+  }
+  out->resize(kept);
+}
+
+WindowPages window_range(const std::vector<PageRef>& list, const TokenWindow& w, int32_t r0, int32_t n_q) {
+  const int32_t hi = std::min(w.t0 + r0 + n_q - 1 + w.ahead, w.n_keys), lo = w.t0 + r0 + 1 - w.window;
+  auto first_where = [&](auto past) {
+    return static_cast<int32_t>(std::partition_point(list.begin(), list.end(), [&](const PageRef& p) {
+             const int32_t start = static_cast<int32_t>(static_cast<uint32_t>(p.n_valid) >> 7);
+             return !past(start, start + (p.n_valid & 127));
+           }) - list.begin());
+  };
+  const int32_t sink_hi = std::min(w.sinks, hi);
+  const int32_t sinks = first_where([&](int32_t start, int32_t) { return start >= sink_hi; });
+  const int32_t from = first_where([&](int32_t, int32_t end) { return end > lo; });
+  const int32_t to = first_where([&](int32_t start, int32_t) { return start >= hi; });
+  if (from >= to) return WindowPages{sinks, 0, sinks};  // sinks alone
+  if (from <= sinks) return WindowPages{to, 0, to};     // one run
+  return WindowPages{sinks, from - sinks, sinks + to - from};
+}
+
 }  // namespace ws

@@ -13,6 +13,8 @@
 #include <string>
 #include <vector>
 
+#include "token_window.hpp"
+
 namespace ws {
 
 struct PageRef {
@@ -36,6 +38,13 @@ struct MaskSpec {
 };
 
 enum class PtStatus { ok, out_of_pages, unknown, committed, shape };
+
+// The pages of a window call's list that rows r0 .. r0 + n_q - 1 of it see: the
+// first `head` entries and, `skip` entries further, the rest of `count`.
+struct WindowPages {
+  int32_t head, skip, count;
+};
+WindowPages window_range(const std::vector<PageRef>& list, const TokenWindow& w, int32_t r0, int32_t n_q);
 
 class PageTable {
  public:
@@ -64,9 +73,13 @@ class PageTable {
   // The same list, appended to *out (for the concatenated lists of a call
   // whose queries belong to several units).
   void visible_pages_append(const MaskSpec& mask, std::vector<PageRef>* out) const;
-  // The visible pages ordered by unit, then kind, then token (appended to *out):
-  // the timeline of a token window; returns its token count.
+  // A token window's timeline: the visible tokens ordered by unit, then kind, then
+  // position.  Its length, its pages (appended to *out; the same length), and of
+  // those the pages that some of n_q rows from w.t0 on see, as list entries of
+  // valid tokens | first index << 7.
+  int64_t timeline_tokens(const MaskSpec& mask) const;
   int64_t timeline_pages(const MaskSpec& mask, std::vector<PageRef>* out) const;
+  void window_pages(const MaskSpec& mask, const TokenWindow& w, int32_t n_q, std::vector<PageRef>* out) const;
   static bool segment_visible(const Segment& s, const MaskSpec& mask);
 
  private:

@@ -70,7 +70,7 @@ __device__ __forceinline__ u32x2 quantise8(const float (&x)[8], float s, float i
       const float e = fmaf(-q, s, x[i]);
       q += e > half ? 1.f : e < -half ? -1.f : 0.f;
       norm2 = fmaf(q, q, norm2);
-      c[i] = static_cast<uint32_t>(static_cast<int>(q));
+      c[i] = static_cast<uint32_t>(static_cast<int>(q) + 128);
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {

@@ -12,7 +12,7 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 // Two codes (the low or high half of a word) as packed bf16(code * scale).
 //   e4m3: the conversion multiplies by the scale, a power of two: exact.
-//   int8: as biased bytes b = code + 128 behind 0x64, a half is 1024 + b; in fp32
+//   int8: bytes b = code + 128 behind 0x64: a half is 1024 + b; in fp32
 //         (1024 + b) s - 1152 s = code s, exact because s has 16 significant
 //         bits; then one rounding.  (A half per perm, a mixed fma each, one pack:
 //         2 instructions a value; through v_cvt_f32_ubyte it is 2.5.)
@@ -23,16 +23,12 @@ template <int kFmt>
 __device__ __forceinline__ QuantScale quant_scale(float s) {
   return QuantScale{s, kFmt == kFmtInt8 ? -1152.0f * s : 0.f};
 }
-template <int kFmt>
-__device__ __forceinline__ uint32_t code_bias(uint32_t w) {
-  return kFmt == kFmtInt8 ? w ^ 0x80808080u : w;
-}
 template <int kFmt, int kHalf>
-__device__ __forceinline__ uint32_t codes_to_bf16(uint32_t biased, const QuantScale& q) {
+__device__ __forceinline__ uint32_t codes_to_bf16(uint32_t codes, const QuantScale& q) {
   if constexpr (kFmt == kFmtE4m3) {
-    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(biased, q.s, kHalf == 1));
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, q.s, kHalf == 1));
   } else {
-    const uint32_t p = __builtin_amdgcn_perm(0x64646464u, biased, kHalf ? 0x04030402u : 0x04010400u);
+    const uint32_t p = __builtin_amdgcn_perm(0x64646464u, codes, kHalf ? 0x04030402u : 0x04010400u);
     const f16x2 h = __builtin_bit_cast(f16x2, p);
     return pack_bf16(fmaf(static_cast<float>(h[0]), q.s, q.c), fmaf(static_cast<float>(h[1]), q.s, q.c));
   }
@@ -40,9 +36,8 @@ __device__ __forceinline__ uint32_t codes_to_bf16(uint32_t biased, const QuantSc
 // Eight codes (two words) as an MFMA operand.
 template <int kFmt>
 __device__ __forceinline__ u32x4 codes8(uint32_t w0, uint32_t w1, const QuantScale& q) {
-  const uint32_t a = code_bias<kFmt>(w0), b = code_bias<kFmt>(w1);
-  return (u32x4){codes_to_bf16<kFmt, 0>(a, q), codes_to_bf16<kFmt, 1>(a, q), codes_to_bf16<kFmt, 0>(b, q),
-                 codes_to_bf16<kFmt, 1>(b, q)};
+  return (u32x4){codes_to_bf16<kFmt, 0>(w0, q), codes_to_bf16<kFmt, 1>(w0, q), codes_to_bf16<kFmt, 0>(w1, q),
+                 codes_to_bf16<kFmt, 1>(w1, q)};
 }
 
 // The keys that the row at timeline index t sees: [lo, hi) and the first `sinks`
@@ -51,7 +46,7 @@ struct RowRange {
   int lo, hi;
 };
 __device__ __forceinline__ RowRange row_range(const TokenWindow& w, int t) {
-  return RowRange{t + 1 - w.window, w.causal ? min(t + 1, w.n_keys) : w.n_keys};
+  return RowRange{t + 1 - w.window, min(t + w.ahead, w.n_keys)};
 }
 __device__ __forceinline__ bool row_sees(const TokenWindow& w, const RowRange& r, int j) {
   return j < r.hi && (j >= r.lo || j < w.sinks);
@@ -67,8 +62,6 @@ __device__ __forceinline__ bool row_sees(const TokenWindow& w, const RowRange& r
 // pages p_begin, p_begin + step, ... (< p_end) of the list; done(i, m, l, o0, o1)
 // takes row i's running maximum (log2), sum and unnormalised pair.
 // ------------------------------------------------------------------------- //
-typedef const __attribute__((address_space(4))) int2* const_page_list;
-
 template <class Page, class Done>
 __device__ __forceinline__ void window_rows_plain(const AttnArgs& a, int head, int row0, int n, int p_begin, int p_end,
                                                   int step, int lane, Page&& page_at, Done&& done) {

@@ -8,6 +8,7 @@
 #include <utility>
 
 #include "device_common.hpp"
+#include "quant_device.hpp"
 #include "ws_kernels.hpp"
 
 namespace ws {
@@ -40,6 +41,20 @@ namespace {
 // 1950; 64 rows per wave halve the LDS operand reads; a row-sum MFMA costs
 // less than the 16 v_dot2 it replaces.)
 // ------------------------------------------------------------------------- //
+
+// What a video kernel reads: pages of which format, and whether a token window may
+// hide keys of a page from some rows.  Paths other than PlainPath take queries of
+// any mode and no rider rows.
+template <int kFormat, bool kWindow>
+struct Path {
+  static constexpr int kFmt = kFormat;
+  static constexpr bool k8 = kFormat != kFmtBf16;
+  static constexpr bool kWin = kWindow;
+  static constexpr bool kPlain = kFormat == kFmtBf16 && !kWindow;
+};
+using PlainPath = Path<kFmtBf16, false>;
+template <int>
+struct Nothing {};
 
 // f(Const<0>), ..., f(Const<N - 1>), unrolled by construction.
 template <int N>
@@ -77,10 +92,6 @@ constexpr uint32_t kStageV = kPageHeadElems * 2;  // offset of the V tile
 __shared__ __attribute__((aligned(1024))) uint16_t g_stages[kStages * 2 * kPageHeadElems];
 
 __device__ __forceinline__ bf16x8 as_bf16x8(u32x4 v) { return __builtin_bit_cast(bf16x8, v); }
-
-// Read-only for a whole launch: accessed through the constant address space
-// so that uniform reads become scalar loads.
-typedef const __attribute__((address_space(4))) int2* const_page_list;
 
 // The call's visible page list: in device memory, or in the kernel
 // arguments themselves (the kernel's only argument is the AttnArgs, at the
@@ -152,7 +163,21 @@ __device__ __forceinline__ void mfma_drain() {
 // What one page's iteration addresses, computed a little at a time during the
 // iteration before it, so that the page boundary holds nothing but the
 // barrier.
-struct PageCtx {
+//
+// 8-bit pages come through registers instead: the loads of the page three ahead
+// go out as the codes of the page two ahead are turned to bf16 and written to its
+// stage, part by part.
+struct Ctx8 {
+  uint32_t ks, vs;         // scales (bits) of the page two ahead (its codes are in the registers)
+  uint32_t ks_load, vs_load;  // of the page three ahead
+  uint32_t wk, wv;         // LDS offsets of this lane's writes of the page two ahead
+};
+struct CtxWin {
+  int start;               // the page's first timeline index
+  int edge;                // some row of the wave does not see all 64 slots
+};
+template <class P>
+struct PageCtx : std::conditional_t<P::k8, Ctx8, Nothing<0>>, std::conditional_t<P::kWin, CtxWin, Nothing<1>> {
   uint32_t k[4];        // LDS offsets of this lane's operand reads: K, per k-step (key tile t: + 4096 t)
   uint32_t v;           // V^T chunk 0 (d tile dt: + 2048 dt)
   uint32_t vp;          // V^T chunk 1 of the page before
@@ -168,7 +193,22 @@ struct PageCtx {
 // of two units out of a window of 128, read with v_readlane, so that the page
 // loop has no scalar load to wait for (scalar loads and LDS reads share a
 // counter that only a full wait can order).
-struct VideoStream {
+struct Stream8 {
+  u32x4 raw[4];          // codes of the page two ahead: K dims 0-63 and 64-127, V dims 0-63 and 64-127
+  uint32_t ks[2], vs[2]; // scales (bits) of the window's units
+  const float* kscale;
+  const float* vscale;
+  uint32_t load;         // this lane's source byte offset within 4 KB of a tile
+  uint32_t wk, wv;       // and its write offsets within a stage (first chunk)
+};
+struct StreamWin {
+  int start[2];          // first timeline index of the window's units
+  int head_pages, skip;  // the class's list: head_pages pages, then after `skip` others the rest
+  int hi_all, lo_all;    // keys [lo_all, hi_all) are seen by every row of the wave
+  TokenWindow win;
+};
+template <class P>
+struct VideoStream : std::conditional_t<P::k8, Stream8, Nothing<2>>, std::conditional_t<P::kWin, StreamWin, Nothing<3>> {
   const_page_list pages;
   FastDiv div_pages;
   int num_heads, n_pages, page0, lo, n;
@@ -184,46 +224,84 @@ struct VideoStream {
   int at;                 // stream index of the current page
   uint32_t stage;         // its stage's LDS offset
   uint32_t valid;         // valid tokens of pages at .. at + 3, a byte each
-  PageCtx c;              // the current page's context
+  PageCtx<P> c;           // the current page's context
 };
 
 // (Past the end: the last unit's entry.  No lane-dependent branch here or
 // anywhere else inside the page loops' regions: with one, the compiler
 // serialises the uniform branches around it and keeps the accumulators of both
 // sides.)
-__device__ __forceinline__ uint32_t stream_entry(const VideoStream& s, int k) {
+// Place in the page list of page `at` of the class's pages.
+template <class P>
+__device__ __forceinline__ int stream_place(const VideoStream<P>& s, int at) {
+  if constexpr (P::kWin) at += at >= s.head_pages ? s.skip : 0;
+  return s.page0 + at;
+}
+// A list entry's valid tokens; with a window its first timeline index.
+template <class P>
+__device__ __forceinline__ uint32_t valid_of(int y) {
+  return P::kWin ? static_cast<uint32_t>(y) & 127u : static_cast<uint32_t>(y);
+}
+__device__ __forceinline__ int start_of(int y) { return static_cast<int>(static_cast<uint32_t>(y) >> 7); }
+template <class P>
+__device__ __forceinline__ uint32_t stream_entry(const VideoStream<P>& s, int k, int* start = nullptr) {
   const uint32_t x = s.lo + min(k, s.n - 1), head = fast_div(x, s.div_pages);
-  const int pi = s.page0 + static_cast<int>(x - head * s.n_pages);
-  return ((s.pages[pi].x * s.num_heads + head) << 7) | static_cast<uint32_t>(s.pages[pi].y);
+  const int pi = stream_place(s, static_cast<int>(x - head * s.n_pages));
+  const int y = s.pages[pi].y;
+  if (start) *start = start_of(y);
+  return ((s.pages[pi].x * s.num_heads + head) << 7) | valid_of<P>(y);
 }
 // The first window: its list entries requested, then combined.
-__device__ __forceinline__ void stream_request(VideoStream& s) {
+template <class P>
+__device__ __forceinline__ void stream_request(VideoStream<P>& s) {
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     const uint32_t x = s.lo + min(64 * k + s.lane, s.n - 1), head = fast_div(x, s.div_pages);
-    const int pi = s.page0 + static_cast<int>(x - head * s.n_pages);
+    const int pi = stream_place(s, static_cast<int>(x - head * s.n_pages));
     s.raw_head[k] = head;
     s.raw_page[k] = s.pages[pi].x;
     s.raw_valid[k] = s.pages[pi].y;
   }
 }
-__device__ __forceinline__ void stream_combine(VideoStream& s) {
+template <class P>
+__device__ __forceinline__ void stream_combine(VideoStream<P>& s) {
 #pragma unroll
-  for (int k = 0; k < 2; ++k)
-    s.ent[k] = ((s.raw_page[k] * s.num_heads + s.raw_head[k]) << 7) | static_cast<uint32_t>(s.raw_valid[k]);
+  for (int k = 0; k < 2; ++k) {
+    s.ent[k] = ((s.raw_page[k] * s.num_heads + s.raw_head[k]) << 7) | valid_of<P>(s.raw_valid[k]);
+    if constexpr (P::kWin) s.start[k] = start_of(s.raw_valid[k]);
+  }
 }
-// Entry of stream index k (uniform, inside the window).
-__device__ __forceinline__ uint32_t stream_peek(const VideoStream& s, int k) {
-  const uint32_t e0 = __builtin_amdgcn_readlane(s.ent[0], k & 63), e1 = __builtin_amdgcn_readlane(s.ent[1], k & 63);
-  return (k & 64) ? e1 : e0;
+// A value of stream index k (uniform, inside the window), from the lanes' two.
+template <class T>
+__device__ __forceinline__ T peek_lanes(const T (&v)[2], int k) {
+  const uint32_t w0 = __builtin_bit_cast(uint32_t, v[0]), w1 = __builtin_bit_cast(uint32_t, v[1]);
+  const uint32_t e0 = __builtin_amdgcn_readlane(w0, k & 63), e1 = __builtin_amdgcn_readlane(w1, k & 63);
+  return __builtin_bit_cast(T, (k & 64) ? e1 : e0);
+}
+// Entry of stream index k.
+template <class P>
+__device__ __forceinline__ uint32_t stream_peek(const VideoStream<P>& s, int k) {
+  return peek_lanes(s.ent, k);
 }
 // Moves the window when the page to look up next, at + 4, enters a new half:
 // it replaces the half that lies two behind.
-__device__ __forceinline__ void stream_reach(VideoStream& s) {
+template <class P>
+__device__ __forceinline__ void stream_reach(VideoStream<P>& s) {
   const int k = s.at + 4;
   if ((k & 63) == 0 && k >= 128) {
-    uint32_t e = stream_entry(s, k + s.lane);
+    int start = 0;
+    uint32_t e = stream_entry(s, k + s.lane, P::kWin ? &start : nullptr);
     asm volatile("" : "+v"(e));  // waited for here, not at every later use
+    if constexpr (P::kWin) {
+      asm volatile("" : "+v"(start));
+      if (k & 64) s.start[1] = start; else s.start[0] = start;
+    }
+    if constexpr (P::k8) {
+      uint32_t ks = __float_as_uint(s.kscale[e >> 7]), vs = __float_as_uint(s.vscale[e >> 7]);
+      asm volatile("" : "+v"(ks), "+v"(vs));
+      if (k & 64) s.ks[1] = ks; else s.ks[0] = ks;
+      if (k & 64) s.vs[1] = vs; else s.vs[0] = vs;
+    }
     if (k & 64) s.ent[1] = e; else s.ent[0] = e;
   }
 }
@@ -261,8 +339,8 @@ __device__ __forceinline__ void dma16(const uint16_t* sbase, uint32_t voff, uint
 // rows 4 wave .. of key tile i (keys 32 (i / 2) + 4 (i % 2) + 8 wave ..); block
 // b of V^T is rows d = 8 b .. 8 b + 7.
 constexpr int kDmaPerPage = 8;  // direct loads per wave and page
-template <int kPart>            // 0..3: K blocks, 4..7: V blocks
-__device__ __forceinline__ void issue_load(const VideoStream& s, const PageCtx& c) {
+template <int kPart, class P>   // 0..3: K blocks, 4..7: V blocks
+__device__ __forceinline__ void issue_load(const VideoStream<P>& s, const PageCtx<P>& c) {
   if constexpr (kPart < 4) {
     constexpr uint32_t src = 2u * k_tile_index(32 * (kPart >> 1) + 4 * (kPart & 1), 0);
     dma16<4096u * kPart>(c.ldk, s.dma_k + src, c.lds);
@@ -271,16 +349,53 @@ __device__ __forceinline__ void issue_load(const VideoStream& s, const PageCtx& 
     dma16<kStageV + 4096u * (kPart - 4)>(c.ldv, s.dma_v + src, c.lds);
   }
 }
-__device__ __forceinline__ void issue_page(const VideoStream& s, const PageCtx& c) {
+template <class P>
+__device__ __forceinline__ void issue_page(const VideoStream<P>& s, const PageCtx<P>& c) {
   static_for<kDmaPerPage>([&](auto i) __attribute__((always_inline)) { issue_load<decltype(i)::value>(s, c); });
 }
-// The load part of a context: the page with entry e into ring stage `stage`.
-__device__ __forceinline__ void set_load(const VideoStream& s, uint32_t e, uint32_t stage, PageCtx& c) {
-  const uint64_t off = static_cast<uint64_t>(e >> 7) << 14;  // 16 KB tiles
+// The load part of a context: the page with entry e (8 bit: loaded to registers;
+// else into ring stage `stage`).
+constexpr uint32_t kCodeTileShift = 13;  // 8 KB of codes
+template <class P>
+__device__ __forceinline__ void set_load(const VideoStream<P>& s, uint32_t e, uint32_t stage, PageCtx<P>& c) {
+  const uint64_t off = static_cast<uint64_t>(e >> 7) << (P::k8 ? kCodeTileShift : 14);  // 16 KB tiles
   c.ldk = reinterpret_cast<const uint16_t*>(reinterpret_cast<uint64_t>(s.kpool) + off);
   c.ldv = reinterpret_cast<const uint16_t*>(reinterpret_cast<uint64_t>(s.vpool) + off);
   c.lds = __builtin_amdgcn_readfirstlane(s.lds0 + stage);
 }
+
+// 8-bit pages.  A thread takes four 16-byte parts of a page (K: dims 64 i + 16 (t %
+// 4) .. of key t / 4; V^T: keys 16 (t % 4) .. of dim 64 i + t / 4; t the thread),
+// two 16-byte chunks of an LDS tile each.  One word of bf16 at a time: word n of 32
+// is word n % 8 of part n / 8; a full chunk is written, a part whose codes are all
+// used is loaded again (of the page three ahead).
+template <int kPart, class P>
+__device__ __forceinline__ void load_part(VideoStream<P>& s, const PageCtx<P>& c) {
+  // (global: a flat load would count among the LDS accesses too)
+  const uint64_t base = reinterpret_cast<uint64_t>(kPart < 2 ? c.ldk : c.ldv) + 4096 * (kPart & 1);
+  s.raw[kPart] = *(const __attribute__((address_space(1))) u32x4*)(base + s.load);
+}
+template <int kWord, bool kAgain, class P>
+__device__ __forceinline__ void stage_word(VideoStream<P>& s, const PageCtx<P>& c, u32x4& chunk) {
+  constexpr int part = kWord >> 3, h = (kWord >> 2) & 1;
+  const QuantScale q = quant_scale<P::kFmt>(__uint_as_float(part < 2 ? c.ks : c.vs));
+  uint32_t w = codes_to_bf16<P::kFmt, kWord & 1>(s.raw[part][(kWord & 7) >> 1], q);
+  asm volatile("" : "+v"(w));
+  chunk[kWord & 3] = w;
+  if constexpr ((kWord & 3) == 3) {
+    const uint32_t at = part < 2 ? (c.wk ^ (16u * h) ^ (128u * (part & 1))) : (c.wv ^ (16u * h)) + 8192u * (part & 1);
+    *(__attribute__((address_space(3))) u32x4*)at = chunk;
+  }
+  if constexpr (kAgain && (kWord & 7) == 7) load_part<part>(s, c);
+}
+template <bool kAgain, class P>
+__device__ __forceinline__ void stage_page(VideoStream<P>& s, const PageCtx<P>& c) {
+  u32x4 chunk;
+  static_for<32>([&](auto n) __attribute__((always_inline)) { stage_word<decltype(n)::value, kAgain>(s, c, chunk); });
+}
+// Waits for the wave's LDS accesses, all or all but the last three.
+__device__ __forceinline__ void wait_lds() { __builtin_amdgcn_s_waitcnt(0xC07F); }
+__device__ __forceinline__ void wait_lds_but_3() { __builtin_amdgcn_s_waitcnt(0xC37F); }
 
 // Waits for this wave's direct loads of every page but the one issued last
 // (loads retire in order).  The barrier that follows then makes every wave's
@@ -304,20 +419,37 @@ template <class T>
 __device__ __forceinline__ void pin_v(T& x) { asm volatile("" : "+v"(x)); }
 
 // The rest of a context: operand reads of the page in ring stage `stage`.
-__device__ __forceinline__ void set_reads(const VideoStream& s, uint32_t stage, PageCtx& c) {
+template <class P>
+__device__ __forceinline__ void set_reads(const VideoStream<P>& s, uint32_t stage, PageCtx<P>& c) {
 #pragma unroll
   for (int n = 0; n < 4; ++n) c.k[n] = (s.k_read + stage) ^ (64u * n);
   c.v = s.v_read + stage;
   c.vp = (s.v_read + ring_add(stage, kStages - 1)) ^ 64u;
 }
 
+// Whether some row of the wave does not see all of a page.
+template <class P>
+__device__ __forceinline__ int page_edge(const VideoStream<P>& s, int start, int valid) {
+  const int end = start + kPageTokens;
+  const int e = (valid < kPageTokens) | (end > s.hi_all) | ((start < s.lo_all) & (end > s.win.sinks));
+  return __builtin_amdgcn_readfirstlane(e);
+}
+
 // Starts the stream: key norms of its first window, the loads of its first
 // three pages, and the context of its first page.  (Past a stream's end the
 // last page is loaded once more, into a stage nothing reads.)
-__device__ __forceinline__ void stream_start(const AttnArgs& a, VideoStream& s) {
+template <class P>
+__device__ __forceinline__ void stream_start(const AttnArgs& a, VideoStream<P>& s) {
   stream_combine(s);
 #pragma unroll
   for (int k = 0; k < 2; ++k) s.kn2[k] = a.knorm2[s.ent[k] >> 7];  // (past the end: the last unit's)
+  if constexpr (P::k8) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      s.ks[k] = __float_as_uint(a.kscale[s.ent[k] >> 7]);
+      s.vs[k] = __float_as_uint(a.vscale[s.ent[k] >> 7]);
+    }
+  }
   if (s.n == 0) return;
   s.valid = 0;
 #pragma unroll
@@ -325,7 +457,24 @@ __device__ __forceinline__ void stream_start(const AttnArgs& a, VideoStream& s) 
     const uint32_t e = stream_peek(s, min(k, s.n - 1));
     s.valid |= (e & 127u) << (8 * k);
     set_load(s, e, k * kStageBytes, s.c);
-    if (k < 3) issue_page(s, s.c);
+    if constexpr (P::k8) {  // pages 0 and 1 to their stages, page 2 to the registers
+      s.c.ks_load = peek_lanes(s.ks, min(k, s.n - 1));
+      s.c.vs_load = peek_lanes(s.vs, min(k, s.n - 1));
+      if (k < 3) {
+        static_for<4>([&](auto i) __attribute__((always_inline)) { load_part<decltype(i)::value>(s, s.c); });
+        s.c.ks = s.c.ks_load;
+        s.c.vs = s.c.vs_load;
+        s.c.wk = s.wk + k * kStageBytes;
+        s.c.wv = s.wv + k * kStageBytes;
+        if (k < 2) stage_page<false>(s, s.c);
+      }
+    } else {
+      if (k < 3) issue_page(s, s.c);
+    }
+  }
+  if constexpr (P::kWin) {
+    s.c.start = peek_lanes(s.start, 0);
+    s.c.edge = page_edge(s, s.c.start, static_cast<int>(s.valid & 127u));
   }
   set_reads(s, 0, s.c);
 }
@@ -344,10 +493,14 @@ struct VideoState {
   bf16x8 ring[4];     // operands in flight (slot = step % 4)
   // rows under a running maximum
   bool any_lazy;      // some row of the wave is one
+  int t_row;          // (windows) timeline index of the lane's row of subtile 0
+  bool any_unset;     // (windows) some such row has met no key it sees: m = kUnset
   uint32_t raised;    // subtiles whose O and l wait to be scaled (bit j) ...
   float scale[kQT];   // ... by this, row q
   u32x4 ones;         // bf16 ones (an opaque value: not rematerialised in front of an MFMA)
 };
+// The running maximum of a row that has met no key it sees; its S tiles start at 0.
+constexpr float kUnset = 3.0e38f;
 // Operand reads are issued this many steps ahead.  (Six, through eight
 // registers, gives the narrower waves nothing: they are not latency-bound.)
 constexpr int kRingAhead = 3;
@@ -430,12 +583,22 @@ __device__ __forceinline__ void scale_raised(VideoState<kQT>& st) {
 // 170.  (A shift fixed at 16 below the logit bound took 154 up to 4, but rounded
 // the largest weight, and out of its reach, from 5 on, the range ran unpipelined
 // under a running maximum: 344 to 455.)
-template <int kQT, bool kFirst, bool kLazy>
-__device__ __forceinline__ void video_iter(VideoState<kQT>& st, VideoStream& s) {
+//
+// 8-bit pages: beside them, a word of bf16 per step (two in the first four; stage_word)
+// turns the codes of page p + 2 into its stage, steps 0-27; the operand reads of
+// steps 28-31 follow the last write, so a wait for all but the wave's last three LDS
+// accesses ends the page.
+// Windows: what hides keys is a page's edge flag, the wave's own.  A row may meet
+// its first visible key late: until then its m is unset and its S the bare logits.
+template <int kQT, bool kFirst, bool kLazy, class P>
+__device__ __forceinline__ void video_iter(VideoState<kQT>& st, VideoStream<P>& s) {
   const int n_valid = static_cast<int>(s.valid & 0xffu);
-  const bool tail = n_valid < kPageTokens;
-  const PageCtx c = s.c;
-  PageCtx nx;
+  const PageCtx<P> c = s.c;
+  bool tail;
+  if constexpr (P::kWin) tail = c.edge != 0;
+  else tail = n_valid < kPageTokens;
+  PageCtx<P> nx;
+  [[maybe_unused]] u32x4 chunk;
   pin_queries(st);
   pin_v(st.ones);
   page_barrier();
@@ -504,6 +667,28 @@ __device__ __forceinline__ void video_iter(VideoState<kQT>& st, VideoStream& s) 
   auto raise = [&](auto ac) __attribute__((always_inline)) {
     constexpr int a = decltype(ac)::value;
     st.raised = 0;
+    if constexpr (P::kWin) {
+      bool unset = false;
+#pragma unroll
+      for (int j = 0; j < kQT; ++j) {
+        const float row = pair_max<32>(pair_max<16>(cm[j]));
+        const bool first = st.m[j] == kUnset && row > -kUnset;  // (O and l are 0)
+        const bool up_row = first || (st.m[j] != kUnset && row > kRaiseAbove);
+        if (__any(up_row)) {
+          const float up = up_row ? row : 0.f;
+          st.raised |= 1u << j;
+          st.scale[j] = first ? 1.f : fast_exp2(-up);
+          st.m[j] = first ? row : st.m[j] == kUnset ? kUnset : st.m[j] + up;
+          const float neg = st.m[j] == kUnset ? 0.f : -st.m[j];
+          st.s_init[j] = (f32x4){neg, neg, neg, neg};
+          sa[a][j] -= up;
+          sa[a + 1][j] -= up;
+        }
+        unset = unset || st.m[j] == kUnset;
+      }
+      st.any_unset = __any(unset);
+      return;
+    }
 #pragma unroll
     for (int j = 0; j < kQT; ++j) {
       const float row = pair_max<32>(pair_max<16>(cm[j]));
@@ -526,20 +711,41 @@ __device__ __forceinline__ void video_iter(VideoState<kQT>& st, VideoStream& s) 
       // logits of slots at or past n_valid become -inf, so they weigh exactly
       // 0 (a correction subtracted from the row sum afterwards would cancel
       // for rows whose logits all sit far below the shift)
-      const int lim = n_valid - 8 * (opaque(s.lane) >> 4);
+      const int off = 8 * (opaque(s.lane) >> 4);
+      const int lim = n_valid - off;
+      if constexpr (P::kWin) {
+        // row by row: keys at or past hi, and from the sinks' end up to lo, are hidden
 #pragma unroll
-      for (int t = a; t < a + 2; ++t)
+        for (int j = 0; j < kQT; ++j) {
+          const RowRange rr = row_range(s.win, st.t_row + 16 * j);
+          const int hi = min(lim, rr.hi - c.start - off), sk = s.win.sinks - c.start - off;
+          const uint32_t hidden = max(rr.lo - s.win.sinks, 0);
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
+          for (int t = a; t < a + 2; ++t)
 #pragma unroll
-          for (int j = 0; j < kQT; ++j)
-            sa[t][j][r] = 32 * (t >> 1) + 4 * (t & 1) + r >= lim ? kNegInf : sa[t][j][r];
+            for (int r = 0; r < 4; ++r) {
+              const int slot = 32 * (t >> 1) + 4 * (t & 1) + r;
+              const bool hide = (slot >= hi) | (static_cast<uint32_t>(slot - sk) < hidden);
+              sa[t][j][r] = hide ? kNegInf : sa[t][j][r];
+            }
+        }
+      } else {
+#pragma unroll
+        for (int t = a; t < a + 2; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int j = 0; j < kQT; ++j)
+              sa[t][j][r] = 32 * (t >> 1) + 4 * (t & 1) + r >= lim ? kNegInf : sa[t][j][r];
+      }
       if constexpr (kLazy) take_all(ac);
     }
     if constexpr (kFirst) {
       if (st.any_lazy) {
         take_all(ac);
-        if constexpr (a == 0) {
+        if constexpr (P::kWin) {
+          raise(ac);
+        } else if constexpr (a == 0) {
 #pragma unroll
           for (int j = 0; j < kQT; ++j) {
             // (a page's first chunk has a valid key; clamped all the same)
@@ -556,7 +762,9 @@ __device__ __forceinline__ void video_iter(VideoState<kQT>& st, VideoStream& s) 
         }
       }
     } else if constexpr (kLazy) {
-      if (__any(top > kRaiseAbove)) raise(ac);
+      bool look = __any(top > kRaiseAbove);
+      if constexpr (P::kWin) look = look || st.any_unset;
+      if (look) raise(ac);
     }
     sched_fence();
   };
@@ -574,15 +782,31 @@ __device__ __forceinline__ void video_iter(VideoState<kQT>& st, VideoStream& s) 
       pin_s(ent);
     }
     if constexpr (o == 15) { st_next = ring_add(s.stage, 1); pin_s(st_next); }
+    constexpr uint32_t tile_shift = P::k8 ? kCodeTileShift : 14;
     if constexpr (o == 16) {
-      nx.ldk = reinterpret_cast<const uint16_t*>(reinterpret_cast<uint64_t>(s.kpool) + (static_cast<uint64_t>(ent >> 7) << 14));
+      nx.ldk = reinterpret_cast<const uint16_t*>(reinterpret_cast<uint64_t>(s.kpool) + (static_cast<uint64_t>(ent >> 7) << tile_shift));
       pin_s(nx.ldk);
     }
     if constexpr (o == 17) {
-      nx.ldv = reinterpret_cast<const uint16_t*>(reinterpret_cast<uint64_t>(s.vpool) + (static_cast<uint64_t>(ent >> 7) << 14));
+      nx.ldv = reinterpret_cast<const uint16_t*>(reinterpret_cast<uint64_t>(s.vpool) + (static_cast<uint64_t>(ent >> 7) << tile_shift));
       pin_s(nx.ldv);
     }
-    if constexpr (o == 18) { nx.lds = s.lds0 + ring_add(st_next, 3); pin_s(nx.lds); }
+    if constexpr (P::k8) {
+      if constexpr (o == 15) {
+        nx.ks = c.ks_load;
+        nx.vs = c.vs_load;
+      }
+      if constexpr (o == 16) { nx.ks_load = peek_lanes(s.ks, look); pin_s(nx.ks_load); }
+      if constexpr (o == 17) { nx.vs_load = peek_lanes(s.vs, look); pin_s(nx.vs_load); }
+      if constexpr (o == 18) { nx.wk = s.wk + ring_add(st_next, 2); pin_v(nx.wk); }
+      if constexpr (o == 19) { nx.wv = s.wv + ring_add(st_next, 2); pin_v(nx.wv); }
+    } else {
+      if constexpr (o == 18) { nx.lds = s.lds0 + ring_add(st_next, 3); pin_s(nx.lds); }
+    }
+    if constexpr (P::kWin) {
+      if constexpr (o == 25) { nx.start = peek_lanes(s.start, min(s.at + 1, s.n - 1)); pin_s(nx.start); }
+      if constexpr (o == 26) { nx.edge = page_edge(s, nx.start, static_cast<int>((s.valid >> 8) & 0xffu)); }
+    }
     if constexpr (o == 19) { nx.k[0] = s.k_read + st_next; pin_v(nx.k[0]); }
     if constexpr (o == 20) { nx.k[1] = nx.k[0] ^ 64u; pin_v(nx.k[1]); }
     if constexpr (o == 21) { nx.k[2] = nx.k[0] ^ 128u; pin_v(nx.k[2]); }
@@ -645,7 +869,16 @@ __device__ __forceinline__ void video_iter(VideoState<kQT>& st, VideoStream& s) 
         else if constexpr (o > 28 && (o & 1)) pack_x(Const<k>{}, Const<o - 9>{});
       }
       if constexpr (last) {
-        if constexpr (o < kDmaPerPage) issue_load<o>(s, c);
+        if constexpr (P::k8) {
+          if constexpr (o < 4) {
+            stage_word<2 * o, true>(s, c, chunk);
+            stage_word<2 * o + 1, true>(s, c, chunk);
+          } else if constexpr (o < 28) {
+            stage_word<o + 4, true>(s, c, chunk);
+          }
+        } else if constexpr (o < kDmaPerPage) {
+          issue_load<o>(s, c);
+        }
         next_ctx(oc);
         if constexpr (o == 14 || o == 30) pin_v(st.ones);
       }
@@ -663,7 +896,8 @@ __device__ __forceinline__ void video_iter(VideoState<kQT>& st, VideoStream& s) 
   // After a range's first page everything is waited for: a load the compiler
   // knows of and believes in flight on entry to the page loop would be waited
   // for in every iteration, with all the direct loads behind it.
-  if constexpr (kFirst) wait_dma_all();
+  if constexpr (P::k8) wait_lds_but_3();
+  else if constexpr (kFirst) wait_dma_all();
   else wait_dma_all_but_last_page();
   s.c = nx;
   s.at += 1;
@@ -673,8 +907,8 @@ __device__ __forceinline__ void video_iter(VideoState<kQT>& st, VideoStream& s) 
 
 // Finishes the last page of a range (its stage is the one before the
 // stream's current): tile 3's exponentials, then the P*V of chunk 1.
-template <int kQT>
-__device__ __forceinline__ void video_flush(VideoState<kQT>& st, const VideoStream& s) {
+template <int kQT, class P>
+__device__ __forceinline__ void video_flush(VideoState<kQT>& st, const VideoStream<P>& s) {
   const uint32_t v1 = s.c.vp;
   mfma_drain();
 #pragma unroll
@@ -707,6 +941,8 @@ struct VideoSeg {
   bool whole;
 };
 
+// How a kernel's queries come: to be normed or scaled, prepared, or as the call says.
+constexpr int kQueriesRaw = 0, kQueriesPrepared = 1, kQueriesAny = 2;
 // A wave's query rows as the call gives them: raw[j][s] = Q[row j][32 s + 8 g .. + 8].
 template <int kQT>
 struct RawQueries {
@@ -715,7 +951,7 @@ struct RawQueries {
   bool ok[kQT];
   int3 pos[kQT];
 };
-template <int kQT, bool kPrepared>
+template <int kQT, int kQueries, class P>
 __device__ __forceinline__ void fetch_queries(const AttnArgs& a, const VideoSeg& sg, int wrow, int lane,
                                               RawQueries<kQT>& x) {
   const int lane_o = opaque(lane), g = lane_o >> 4, i16 = lane_o & 15;
@@ -731,10 +967,10 @@ __device__ __forceinline__ void fetch_queries(const AttnArgs& a, const VideoSeg&
 #pragma unroll
     for (int s = 0; s < 4; ++s) x.raw[j][s] = *reinterpret_cast<const u32x4*>(p + 32 * s);
     x.pos[j] = make_int3(0, 0, 0);
-    if (!kPrepared && a.mode == 1 && x.ok[j])
+    if (kQueries != kQueriesPrepared && a.mode == 1 && x.ok[j])
       x.pos[j] = make_int3(a.positions[3 * row], a.positions[3 * row + 1], a.positions[3 * row + 2]);
   }
-  if (a.n_rq > 0 && wrow + 16 * kQT > a.rq_row0) {  // rider rows among them
+  if (P::kPlain && a.n_rq > 0 && wrow + 16 * kQT > a.rq_row0) {  // rider rows among them
 #pragma unroll
     for (int j = 0; j < kQT; ++j) {
       const int q = wrow + 16 * j + i16 - a.rq_row0;
@@ -749,11 +985,11 @@ __device__ __forceinline__ void fetch_queries(const AttnArgs& a, const VideoSeg&
 }
 
 // The prepared queries, st.q[j][s] = Q''[row j][32 s + 8 g .. + 8], by the
-// call's query mode (kPrepared: 2, given as they are, else 0 or 1); rider rows
+// call's query mode (2: given as they are, else 0 or 1); rider rows
 // (at and past rq_row0) come prepared.
-template <int kQT, bool kPrepared>
+template <int kQT, int kQueries>
 __device__ __forceinline__ void prepare_rows(const AttnArgs& a, const RawQueries<kQT>& x, int g, VideoState<kQT>& st) {
-  if (kPrepared) {
+  if (kQueries == kQueriesPrepared || (kQueries == kQueriesAny && a.mode == 2)) {
 #pragma unroll
     for (int j = 0; j < kQT; ++j)
 #pragma unroll
@@ -821,14 +1057,14 @@ __device__ __forceinline__ void prepare_rows(const AttnArgs& a, const RawQueries
   }
 }
 
-template <int kQT, bool kPrepared>
-__device__ __forceinline__ void video_segment(const AttnArgs& a, const VideoSeg& sg, VideoStream& s, int wave) {
+template <int kQT, int kQueries, class P>
+__device__ __forceinline__ void video_segment(const AttnArgs& a, const VideoSeg& sg, VideoStream<P>& s, int wave) {
   const int wrow = sg.q_lo + wave * 16 * kQT;
   VideoState<kQT> st;
   {
     RawQueries<kQT> raw;
-    fetch_queries<kQT, kPrepared>(a, sg, wrow, s.lane, raw);
-    prepare_rows<kQT, kPrepared>(a, raw, s.lane >> 4, st);
+    fetch_queries<kQT, kQueries, P>(a, sg, wrow, s.lane, raw);
+    prepare_rows<kQT, kQueries>(a, raw, s.lane >> 4, st);
   }
 
   // ---- softmax shift ----
@@ -859,38 +1095,46 @@ __device__ __forceinline__ void video_segment(const AttnArgs& a, const VideoSeg&
     const float bound = sqrtf(pair_sum<32>(pair_sum<16>(qn2)) * kn2);
     const bool is = a.fixed_shift == 0 || bound > kShiftBoundMax;
     lazy = lazy || is;
-    st.m[j] = is ? -1.f : bound;  // (-1: to be set by the first keys)
+    st.m[j] = is ? (P::kWin ? kUnset : -1.f) : bound;  // (-1: to be set by the first keys)
     const float neg = is ? 0.f : -bound;
     st.s_init[j] = (f32x4){neg, neg, neg, neg};
   }
   st.any_lazy = __any(lazy);
+  if constexpr (P::kWin) {
+    st.any_unset = st.any_lazy;
+    st.t_row = a.win.t0 + wrow + (s.lane & 15);
+  }
   st.raised = 0;
   pin_queries(st);
   st.ones = (u32x4){0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
   asm volatile("" : "+v"(st.ones));
 
   // ---- the segment's pages ----
-  if (s.at == 0) wait_dma_all_but_last_page();
+  if constexpr (P::k8) {
+    if (s.at == 0) wait_lds();
+  } else {
+    if (s.at == 0) wait_dma_all_but_last_page();
+  }
   const int end = s.at + sg.n;
-  video_iter<kQT, true, false>(st, s);
+  video_iter<kQT, true, false, P>(st, s);
   // (one-armed branches in turn: of an if-else the compiler keeps both arms'
   // accumulators.  In this order, and with the last scaling in the second arm,
   // the first loop keeps its speed: 40 heads, 920 rows, 139 and 479 pages 132.5 and
   // 443.4 us a step; the other way round 133.8 and 448.0, with the scaling in the
   // flush as well; without the second loop 131.8 and 441.1.)
   if (!st.any_lazy)
-    while (s.at < end) video_iter<kQT, false, false>(st, s);
+    while (s.at < end) video_iter<kQT, false, false, P>(st, s);
   if (st.any_lazy) {
-    while (s.at < end) video_iter<kQT, false, true>(st, s);
+    while (s.at < end) video_iter<kQT, false, true, P>(st, s);
     mfma_drain();
     scale_raised(st);
   }
   video_flush<kQT>(st, s);
-  if (s.at == s.n) wait_dma_all();  // no direct load may still be writing this workgroup's LDS when it exits
+  if (!P::k8 && s.at == s.n) wait_dma_all();  // no direct load may still be writing this workgroup's LDS when it exits
 
   // ---- epilogue: lane holds O^T[16 dt + 4 g + r][q] ----
   const int lane_e = opaque(s.lane), ge = lane_e >> 4, ie = lane_e & 15;
-  const bool riders = a.n_rq > 0 && wrow + 16 * kQT > a.rq_row0;
+  const bool riders = P::kPlain && a.n_rq > 0 && wrow + 16 * kQT > a.rq_row0;
   // bf16: the output itself, or the partial of a key range: the
   // softmax-normalised O (a convex combination of V rows, so bf16 keeps its
   // range; the merge adds at most one more bf16 rounding of the output's size)
@@ -899,6 +1143,32 @@ __device__ __forceinline__ void video_segment(const AttnArgs& a, const VideoSeg&
   uint16_t* const base = sg.whole ? a.out + sg.head * a.out_head_stride
                                   : reinterpret_cast<uint16_t*>(a.part_o) + part_row * kHeadDim;
   const int64_t stride = sg.whole ? a.out_tok_stride : kHeadDim;
+  if constexpr (P::kWin && !P::k8) {
+    // a value that some row does not see may have reached it through a weight of 0
+    uint32_t top = 0;
+#pragma unroll
+    for (int j = 0; j < kQT; ++j)
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) top = max(top, __float_as_uint(st.o[dt][j][r]) << 1);
+    if (__any(top >= 0xff000000u)) {
+      const int first = s.at - sg.n;
+      window_rows_plain(
+          a, sg.head, wrow, min(16 * kQT, sg.q_hi - wrow), 0, sg.n, 1, lane_e,
+          [&](int p) {
+            const uint32_t x = s.lo + first + p;
+            const int pi = stream_place(s, static_cast<int>(x - sg.head * s.n_pages));
+            return make_int2(s.pages[pi].x, s.pages[pi].y);
+          },
+          [&](int i, float m, float l, float o0, float o1) {
+            const float inv = l > 0.f ? 1.0f / l : 0.f;
+            *reinterpret_cast<uint32_t*>(base + (wrow + i) * stride + 2 * lane_e) = pack_bf16(o0 * inv, o1 * inv);
+            if (!sg.whole && lane_e == 0) a.part_lse[part_row + wrow + i] = l > 0.f ? m + __log2f(l) : kNegInf;
+          });
+      return;
+    }
+  }
   uint16_t* const op = base + (wrow + ie) * stride + 16 * (ge & 1) + 8 * (ge >> 1);
 #pragma unroll
   for (int j = 0; j < kQT; ++j) {
@@ -1213,7 +1483,37 @@ __device__ __forceinline__ void rider_rest(const AttnArgs& a, RiderWork& w, int 
 
 // A segment for a wave without query rows: it issues its share of the page
 // loads and attends the rider rows' pages (n_seg > 0: the head's ranges).
-__device__ __forceinline__ void video_idle_segment(const AttnArgs& a, const VideoSeg& sg, VideoStream& s, int n_seg) {
+template <class P>
+__device__ __forceinline__ void video_idle_segment(const AttnArgs& a, const VideoSeg& sg, VideoStream<P>& s, int n_seg) {
+  if constexpr (!P::kPlain) {
+    if (s.at == 0) {
+      if constexpr (P::k8) wait_lds();
+      else wait_dma_all_but_last_page();
+    }
+    for (int k = 0; k < sg.n; ++k) {
+      page_barrier();
+      if constexpr (P::k8) stage_page<true>(s, s.c);
+      else issue_page(s, s.c);
+      const int at = min(s.at + 4, s.n - 1);
+      s.at += 1;
+      s.stage = ring_add(s.stage, 1);
+      if constexpr (P::k8) {
+        s.c.ks = s.c.ks_load;
+        s.c.vs = s.c.vs_load;
+        s.c.ks_load = peek_lanes(s.ks, at);
+        s.c.vs_load = peek_lanes(s.vs, at);
+        s.c.wk = s.wk + ring_add(s.stage, 2);
+        s.c.wv = s.wv + ring_add(s.stage, 2);
+        set_load(s, stream_peek(s, at), 0, s.c);
+        wait_lds();
+      } else {
+        set_load(s, stream_peek(s, at), ring_add(s.stage, 3), s.c);
+        wait_dma_all_but_last_page();
+      }
+      stream_reach(s);
+    }
+    return;
+  }
   RiderWork w;
   w.item = w.n_items = 0;
   w.loaded = false;
@@ -1247,7 +1547,8 @@ struct VideoWork {
   VideoPartition32 part;
   int group, q_lo, q_hi;
 };
-__device__ __forceinline__ VideoSeg video_seg(const VideoWork& w, const VideoStream& s, int k) {
+template <class P>
+__device__ __forceinline__ VideoSeg video_seg(const VideoWork& w, const VideoStream<P>& s, int k) {
   const int x = s.lo + k;
   const int head = static_cast<int>(fast_div(x, s.div_pages)), h0 = head * s.n_pages;
   const int n = min(s.n - k, h0 + s.n_pages - x);
@@ -1256,19 +1557,26 @@ __device__ __forceinline__ VideoSeg video_seg(const VideoWork& w, const VideoStr
 }
 
 // Ranges of a head (for the rider rows' partials).
-__device__ __forceinline__ int head_ranges(const VideoWork& w, const VideoStream& s, int head) {
+template <class P>
+__device__ __forceinline__ int head_ranges(const VideoWork& w, const VideoStream<P>& s, int head) {
   const int h0 = head * s.n_pages;
   return static_cast<int>(part_group_of(w.part, h0 + s.n_pages - 1) - part_group_of(w.part, h0)) + 1;
 }
 
-template <int kQT, bool kPrepared>
-__device__ __forceinline__ void video_wave(const AttnArgs& a, const VideoWork& w, VideoStream& s, int wave) {
+template <int kQT, int kQueries, class P>
+__device__ __forceinline__ void video_wave(const AttnArgs& a, const VideoWork& w, VideoStream<P>& s, int wave) {
+  if constexpr (P::kWin) {
+    const int t_first = a.win.t0 + w.q_lo + wave * 16 * kQT;
+    const int t_last = a.win.t0 + min(w.q_lo + (wave + 1) * 16 * kQT, w.q_hi) - 1;
+    s.hi_all = row_range(s.win, t_first).hi;
+    s.lo_all = row_range(s.win, t_last).lo;
+  }
   stream_start(a, s);
-  while (s.at < s.n) video_segment<kQT, kPrepared>(a, video_seg(w, s, s.at), s, wave);
+  while (s.at < s.n) video_segment<kQT, kQueries, P>(a, video_seg(w, s, s.at), s, wave);
 }
 
 // The rider rows' pages for a wave with rows of its own, after its segments.
-__device__ __forceinline__ void rider_segments(const AttnArgs& a, const VideoWork& w, const VideoStream& s) {
+__device__ __forceinline__ void rider_segments(const AttnArgs& a, const VideoWork& w, const VideoStream<PlainPath>& s) {
   for (int k = 0; k < s.n;) {
     const VideoSeg sg = video_seg(w, s, k);
     RiderWork r;
@@ -1288,8 +1596,7 @@ __device__ __forceinline__ void video_empty(const AttnArgs& a, int head, int q_l
   }
 }
 
-// kPrepared: the video queries come prepared (query mode 2).
-template <bool kPrepared>
+template <class P, int kQueries>
 __device__ __forceinline__ void unit_attn(const AttnArgs& a) {
   // Work decode.  Each query class (the rows of one unit's queries, with the
   // pages its mask leaves visible) owns a block of workgroups: n_groups
@@ -1317,7 +1624,7 @@ __device__ __forceinline__ void unit_attn(const AttnArgs& a) {
   const int q0 = tab[ci].q0, q_hi = q0 + tab[ci].n_q;
   const int tile_rows = tab[ci].tile_rows, q_lo = q0 + qt * tile_rows;
   // rider rows follow the video rows (a single class then)
-  const int row_end = min(q_lo + tile_rows, a.n_rq > 0 ? a.rq_row0 + a.n_rq : q_hi);
+  const int row_end = min(q_lo + tile_rows, P::kPlain && a.n_rq > 0 ? a.rq_row0 + a.n_rq : q_hi);
   const int wave_rows = video_wave_rows(tile_rows, row_end - q_lo);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
 
@@ -1325,9 +1632,19 @@ __device__ __forceinline__ void unit_attn(const AttnArgs& a) {
   w.group = group;
   w.q_lo = q_lo;
   w.q_hi = q_hi;
-  VideoStream s;
+  VideoStream<P> s;
   s.pages = page_list(a);
   s.num_heads = a.num_heads;
+  if constexpr (P::kWin) {
+    s.win = a.win;
+    s.head_pages = tab[ci].head_pages;
+    s.skip = tab[ci].skip;
+    s.hi_all = s.lo_all = 0;  // (a wave without rows asks for no edges)
+  }
+  if constexpr (P::k8) {
+    s.kscale = a.kscale;
+    s.vscale = a.vscale;
+  }
   s.n_pages = tab[ci].n_pages;
   s.page0 = tab[ci].page0;
   s.lane = lane;
@@ -1357,26 +1674,37 @@ __device__ __forceinline__ void unit_attn(const AttnArgs& a) {
     const int d = 8 * wave + (lane >> 3);
     s.dma_v = 2 * v_tile_index(8 * ((lane & 7) ^ ((d >> 1) & 7)), d);
     const uint32_t lds = lds_offset(g_stages);
+    if constexpr (P::k8) {
+      const uint32_t t = 64u * wave + lane, key = t >> 2, part = t & 3;
+      // K: row 16 tile + m of the key, chunks 2 part (and 8 further, and the odd ones)
+      const uint32_t tile = 2 * (key >> 5) + ((key >> 2) & 1), row = 4 * ((key >> 3) & 3) + (key & 3);
+      s.load = 16u * t;
+      s.wk = lds + 256u * (16u * tile + row) + 16u * ((2u * part) ^ row);
+      s.wv = lds + kStageV + 128u * key + 16u * ((2u * part) ^ ((key >> 1) & 7));  // (V^T: dim t / 4)
+    }
     s.lds0 = __builtin_amdgcn_readfirstlane(lds + 1024u * wave);
     const int g = lane >> 4, i16 = lane & 15;
     s.k_read = lds + 256u * i16 + 16u * (g ^ i16);
     s.v_read = lds + kStageV + 128u * i16 + 16u * (g ^ ((i16 >> 1) & 7));
   }
-  const bool rx = a.rx_pages > 0 && qt == n_qtiles - 1 && wave == kVideoWaves - 1;
+  const bool rx = P::kPlain && a.rx_pages > 0 && qt == n_qtiles - 1 && wave == kVideoWaves - 1;
   if (q_lo + wave * wave_rows >= row_end) {
     stream_start(a, s);
     while (s.at < s.n) {
       const VideoSeg sg = video_seg(w, s, s.at);
       video_idle_segment(a, sg, s, rx ? head_ranges(w, s, sg.head) : 0);
     }
-    wait_dma_all();
+    if (!P::k8) wait_dma_all();
     return;
   }
-  if (wave_rows == 64) video_wave<4, kPrepared>(a, w, s, wave);
-  else if (wave_rows == 48) video_wave<3, kPrepared>(a, w, s, wave);
-  else video_wave<2, kPrepared>(a, w, s, wave);
-  if (rx) rider_segments(a, w, s);
+  if (wave_rows == 64) video_wave<4, kQueries>(a, w, s, wave);
+  else if (wave_rows == 48) video_wave<3, kQueries>(a, w, s, wave);
+  else video_wave<2, kQueries>(a, w, s, wave);
+  if constexpr (P::kPlain)
+    if (rx) rider_segments(a, w, s);
 }
+
+#define WS_ONE_WAVE_PER_SIMD __launch_bounds__(kVideoWaves * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
 
 }  // namespace
 }  // namespace ws

@@ -117,7 +117,7 @@ bool same_mask(const ws::MaskSpec& a, const ws::MaskSpec& b) {
 }
 
 bool same_window(const ws::TokenWindow& a, const ws::TokenWindow& b) {
-  return a.on == b.on && a.causal == b.causal && a.t0 == b.t0 && a.window == b.window && a.sinks == b.sinks &&
+  return a.on == b.on && a.ahead == b.ahead && a.t0 == b.t0 && a.window == b.window && a.sinks == b.sinks &&
          a.n_keys == b.n_keys;
 }
 
@@ -488,7 +488,8 @@ float scale_log2_of(float softmax_scale) {
 // One attention call, validated and resolved into launch arguments.
 struct AttnPlan {
   bool audio = false;
-  bool few = false;  // the kernel of 8-bit pages and token windows (quant.hip)
+  bool few = false;   // 8-bit pages or a token window: the kernel of few rows (quant.hip) ...
+  bool path = false;  // ... or the video kernel's form (video_paths.hip)
   ws::AttnArgs a{};
   bool merge = false;
   ws::CombineArgs cb{};
@@ -507,44 +508,61 @@ ws_status refuse_capture(hipStream_t stream) {
   return WS_OK;
 }
 
-constexpr int32_t kMaxTimeline = 1 << 24;  // tokens a window's page entries can index
-constexpr int32_t kMaxWindow = 1 << 30;
+// Rows of a unit attention (8-bit pages) or a window attention that go to the
+// kernel of few rows.
+constexpr int kFewRows = 64;
 
-// The pages of a token window's timeline that some of its n_q rows see, into
-// c->scratch_list (entry: valid | first index << 7), and the kernel's window.
-ws_status window_pages(ws_cache* c, const ws_window_spec& w, int32_t n_q, ws::TokenWindow* out) {
-  std::vector<ws::PageRef>& list = c->scratch_list;
-  list.clear();
-  const int64_t n = c->pt.timeline_pages(
-      ws::MaskSpec{w.mask.q_unit, w.mask.min_visible_unit, w.mask.kind_mask}, &list);
-  if (n > kMaxTimeline)
+// A window call's own part: the segments of its timeline, and the rows' window
+// (t0: of the call's first row).
+struct WindowCall {
+  ws::MaskSpec mask;
+  ws::TokenWindow win;
+  int32_t tile_rows;  // of the video kernel's form
+};
+
+// Checks a window and resolves it against the cache.
+ws_status resolve_window(ws_cache* c, const ws_window_spec& w, int32_t n_q, WindowCall* out) {
+  if (w.window < 0 || w.n_sink < 0)
+    return fail(WS_ERR_INVALID_ARG, "window %d and n_sink %d must be >= 0", w.window, w.n_sink);
+  if (w.causal != 0 && w.causal != 1) return fail(WS_ERR_INVALID_ARG, "causal must be 0 or 1");
+  if (w.q_start < WS_WINDOW_AT_END || w.q_start > ws::kMaxTimeline)
+    return fail(WS_ERR_INVALID_ARG, "q_start %d outside [0, 2^24] and not WS_WINDOW_AT_END", w.q_start);
+  out->mask = ws::MaskSpec{w.mask.q_unit, w.mask.min_visible_unit, w.mask.kind_mask};
+  const int64_t n = c->pt.timeline_tokens(out->mask);
+  if (n > ws::kMaxTimeline)
     return fail(WS_ERR_SHAPE, "timeline of %lld tokens (at most 2^24)", static_cast<long long>(n));
-  ws::TokenWindow t{};
+  ws::TokenWindow& t = out->win;
+  t = ws::TokenWindow{};
   t.on = 1;
-  t.causal = w.causal;
+  t.ahead = w.causal ? 1 : ws::kNoWindow;
   t.n_keys = static_cast<int32_t>(n);
   t.t0 = w.q_start == WS_WINDOW_AT_END ? t.n_keys - n_q : w.q_start;
-  t.window = w.window == 0 ? kMaxWindow : std::min(w.window, kMaxWindow);
+  t.window = w.window == 0 ? ws::kNoWindow : std::min(w.window, ws::kNoWindow);
   t.sinks = std::min(w.n_sink, t.n_keys);
-  // seen by some row: [lo of the first row, hi of the last), and the sinks below
-  const int32_t hi = w.causal ? std::min(t.t0 + n_q, t.n_keys) : t.n_keys;
-  const int32_t lo = t.t0 + 1 - t.window;
-  size_t kept = 0;
-  int32_t start = 0;
-  for (const ws::PageRef p : list) {  // (a copy: the list is rewritten in place)
-    if (start < hi && (start + p.n_valid > lo || start < t.sinks))
-      list[kept++] = ws::PageRef{p.page, p.n_valid | static_cast<int32_t>(static_cast<uint32_t>(start) << 7)};
-    start += p.n_valid;
-  }
-  list.resize(kept);
-  *out = t;
   return WS_OK;
+}
+
+// Query classes of a window call: one per query tile, each over the pages of the
+// call's list that its rows see.
+void window_classes(const std::vector<ws::PageRef>& list, const ws::TokenWindow& w, int32_t n_q, int32_t tile_rows,
+                    ws::AttnArgs* a) {
+  a->n_classes = 0;
+  for (int32_t r0 = 0; r0 < n_q; r0 += tile_rows) {
+    ws::AttnClass& cl = a->cls[a->n_classes++];
+    cl = ws::AttnClass{};
+    cl.q0 = r0;
+    cl.n_q = std::min(tile_rows, n_q - r0);
+    const ws::WindowPages p = ws::window_range(list, w, r0, cl.n_q);
+    cl.head_pages = p.head;
+    cl.skip = p.skip;
+    cl.n_pages = p.count;
+  }
 }
 
 ws_status plan_attention(bool audio, const void* q, int64_t q_tok_stride, int64_t q_head_stride,
                          int32_t n_groups, const QueryGroup* groups, const ws_query_desc* qd, ws_cache* c,
                          void* out, int64_t out_tok_stride, int64_t out_head_stride,
-                         hipStream_t stream, AttnPlan* plan, const ws_window_spec* window = nullptr) {
+                         hipStream_t stream, AttnPlan* plan, const WindowCall* window = nullptr) {
   if (!c || !qd || !groups) return fail(WS_ERR_INVALID_ARG, "NULL argument");
   if (ws_status st = check_device(c); st != WS_OK) return st;
   if (n_groups < 1 || n_groups > (audio ? 1 : ws::kMaxClasses))
@@ -570,23 +588,18 @@ ws_status plan_attention(bool audio, const void* q, int64_t q_tok_stride, int64_
   if (!std::isfinite(qd->softmax_scale) || qd->softmax_scale < 0.f)
     return fail(WS_ERR_INVALID_ARG, "bad softmax_scale");
 
-  if (window) {
-    if (window->window < 0 || window->n_sink < 0)
-      return fail(WS_ERR_INVALID_ARG, "window %d and n_sink %d must be >= 0", window->window, window->n_sink);
-    if (window->causal != 0 && window->causal != 1) return fail(WS_ERR_INVALID_ARG, "causal must be 0 or 1");
-    if (window->q_start < WS_WINDOW_AT_END || window->q_start > kMaxTimeline)
-      return fail(WS_ERR_INVALID_ARG, "q_start %d outside [0, 2^24] and not WS_WINDOW_AT_END", window->q_start);
-  }
-
   // Each group with rows is a query class with its own visible page list;
   // the lists are concatenated.  The whole list goes into the kernel
   // arguments when it fits, else into the device arena (one upload per
   // distinct list).
   plan->audio = audio;
-  plan->few = window || c->format != WS_KV_BF16;
+  const bool special = window || c->format != WS_KV_BF16;
+  plan->few = special && (audio || (n_groups == 1 && n_q <= kFewRows));
+  plan->path = special && !plan->few;
   const bool few_rows = audio || plan->few;  // key ranges of 16-row tiles, merged in fp32
   ws::AttnArgs& a = plan->a;
   a = ws::AttnArgs{};
+  a.win = window ? window->win : ws::TokenWindow{0, ws::kNoWindow, 0, ws::kNoWindow, 0, ws::kNoWindow};
   const int2* plist = nullptr;
   ws::MaskSpec masks[ws::kMaxClasses];
   int n_cls = 0;
@@ -598,11 +611,9 @@ ws_status plan_attention(bool audio, const void* q, int64_t q_tok_stride, int64_
     cl.q0 = r0;
     cl.n_q = groups[g].n_q;
     cl.page0 = static_cast<int32_t>(c->scratch_list.size());
-    if (window) {
-      if (ws_status st = window_pages(c, *window, groups[g].n_q, &a.win); st != WS_OK) return st;
-    } else {
-      c->pt.visible_pages_append(groups[g].mask, &c->scratch_list);
-    }
+    if (window) c->pt.window_pages(window->mask, window->win, n_q, &c->scratch_list);
+    else c->pt.visible_pages_append(groups[g].mask, &c->scratch_list);
+    cl.head_pages = static_cast<int32_t>(c->scratch_list.size()) - cl.page0;
     cl.n_pages = static_cast<int32_t>(c->scratch_list.size()) - cl.page0;
   }
   const int32_t n_pages = static_cast<int32_t>(c->scratch_list.size());
@@ -611,11 +622,15 @@ ws_status plan_attention(bool audio, const void* q, int64_t q_tok_stride, int64_
       a.inline_pages[i] = make_int2(c->scratch_list[static_cast<size_t>(i)].page,
                                     c->scratch_list[static_cast<size_t>(i)].n_valid);
   } else {
-    if (plan->few)
+    if (special)
       if (ws_status st = refuse_capture(stream); st != WS_OK) return st;
     if (ws_status st = arena_list(c, masks, n_cls, a.win, window ? n_q : 0, stream, &plist); st != WS_OK) return st;
   }
   a.n_classes = n_cls;
+  if (window && plan->path) {
+    window_classes(c->scratch_list, a.win, n_q, window->tile_rows, &a);
+    n_cls = a.n_classes;
+  }
   a.q = static_cast<const uint16_t*>(q);
   a.q_tok_stride = q_tok_stride;
   a.q_head_stride = q_head_stride;
@@ -689,8 +704,11 @@ ws_status plan_attention(bool audio, const void* q, int64_t q_tok_stride, int64_
       const int cus = c->opt_class_cus == 1 || n_cls == 1 || work == 0
                           ? c->num_cus
                           : static_cast<int>(std::max<int64_t>(cl.n_qtiles, c->num_cus * w / work));
+      if (window) cl.tile_rows = window->tile_rows;  // (a class is one tile)
       if (c->opt_video_splits > 0 && cl.n_pages > 0) {  // (forced splits keep the full tile)
         cl.n_groups = H * c->opt_video_splits;
+      } else if (window) {
+        cl.n_groups = static_cast<int32_t>(ws::video_group_count(H, 1, cl.n_pages, cus));
       } else {
         const ws::VideoTiling t = ws::video_tiling(H, cl.n_q, cl.n_pages, cus);
         cl.tile_rows = t.rows;
@@ -748,7 +766,8 @@ ws_status plan_attention(bool audio, const void* q, int64_t q_tok_stride, int64_
 
 hipError_t launch_plan_kernel(const AttnPlan& p, hipStream_t stream, hipEvent_t start = nullptr,
                               hipEvent_t stop = nullptr) {
-  return p.few     ? ws::launch_few_attention(p.a, stream, start, stop)
+  return p.path    ? ws::launch_path_attention(p.a, stream, start, stop)
+         : p.few   ? ws::launch_few_attention(p.a, stream, start, stop)
          : p.audio ? ws::launch_audio_attention(p.a, stream, start, stop)
                    : ws::launch_unit_attention(p.a, stream, start, stop);
 }
@@ -778,37 +797,62 @@ ws_status attention_impl(bool audio, const void* q, int64_t q_tok_stride, int64_
                          void* hip_stream) {
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   AttnPlan p;
-  if (c && c->format != WS_KV_BF16 && groups && qd && n_groups > 1) {  // 8-bit pages: one call per group
-    int32_t n_q = 0, last = 0;
-    for (int g = 0; g < n_groups; ++g) {
-      if (groups[g].n_q < 0) return fail(WS_ERR_SHAPE, "query group %d has a negative row count", g);
-      n_q += groups[g].n_q;
-      if (groups[g].n_q > 0) last = g;
-    }
-    if (n_q < 1 || n_q > c->cfg.max_q_tokens)
-      return fail(WS_ERR_SHAPE, "n_q %d out of range [1, %d]", n_q, c->cfg.max_q_tokens);
-    if (ws_status st = check_strides("q", q, q_tok_stride, q_head_stride, n_q, c->cfg.num_heads); st != WS_OK) return st;
-    if (ws_status st = check_strides("out", out, out_tok_stride, out_head_stride, n_q, c->cfg.num_heads); st != WS_OK)
-      return st;
-    int64_t r0 = 0;
-    for (int g = 0; g <= last; r0 += groups[g].n_q, ++g) {
-      if (groups[g].n_q == 0) continue;
-      ws_query_desc d = *qd;
-      if (d.positions) d.positions += 3 * r0;
-      if (ws_status st = attention_impl(audio, static_cast<const uint16_t*>(q) + r0 * q_tok_stride, q_tok_stride,
-                                        q_head_stride, 1, groups + g, &d, c,
-                                        static_cast<uint16_t*>(out) + r0 * out_tok_stride, out_tok_stride,
-                                        out_head_stride, hip_stream);
-          st != WS_OK)
-        return st;
-    }
-    return WS_OK;
-  }
   if (ws_status st = plan_attention(audio, q, q_tok_stride, q_head_stride, n_groups, groups, qd, c, out,
                                     out_tok_stride, out_head_stride, stream, &p);
       st != WS_OK)
     return st;
   return run_plan(c, p, stream);
+}
+
+// A window call: few rows at once, or the video kernel's form in launches of up to
+// kMaxClasses query tiles, each over the pages that its rows see.
+ws_status window_impl(const void* q, int64_t q_tok_stride, int64_t q_head_stride, int32_t n_q, const ws_query_desc* qd,
+                      ws_cache* c, const ws_window_spec* spec, void* out, int64_t out_tok_stride,
+                      int64_t out_head_stride, hipStream_t stream) {
+  if (!c || !qd || !spec) return fail(WS_ERR_INVALID_ARG, "NULL argument");
+  if (n_q < 1 || n_q > c->cfg.max_q_tokens)
+    return fail(WS_ERR_SHAPE, "n_q %d out of range [1, %d]", n_q, c->cfg.max_q_tokens);
+  const int H = c->cfg.num_heads;
+  if (ws_status st = check_strides("q", q, q_tok_stride, q_head_stride, n_q, H); st != WS_OK) return st;
+  if (ws_status st = check_strides("out", out, out_tok_stride, out_head_stride, n_q, H); st != WS_OK) return st;
+  WindowCall w{};
+  if (ws_status st = resolve_window(c, *spec, n_q, &w); st != WS_OK) return st;
+  int32_t launch_rows = n_q;
+  if (n_q > kFewRows) {
+    w.tile_rows = ws::kVideoQTile;
+    if (c->opt_video_splits == 0) {
+      c->scratch_list.clear();
+      c->pt.window_pages(w.mask, w.win, std::min(n_q, ws::kVideoQTile), &c->scratch_list);
+      w.tile_rows = ws::video_tiling(H, n_q, static_cast<int64_t>(c->scratch_list.size()), c->num_cus).rows;
+    }
+    launch_rows = ws::kMaxClasses * w.tile_rows;
+  }
+  const int32_t t0 = w.win.t0;
+  auto launch_at = [&](int32_t r0) {
+    w.win.t0 = t0 + r0;
+    return std::min(launch_rows, n_q - r0);
+  };
+  // (a later launch's refusal comes before the first is enqueued)
+  for (int32_t r0 = 0; n_q > launch_rows && r0 < n_q; r0 += launch_rows) {
+    const int32_t rows = launch_at(r0);
+    c->scratch_list.clear();
+    c->pt.window_pages(w.mask, w.win, rows, &c->scratch_list);
+    if (c->scratch_list.size() > static_cast<size_t>(ws::AttnArgs::kInlinePages))
+      if (ws_status st = refuse_capture(stream); st != WS_OK) return st;
+  }
+  for (int32_t r0 = 0; r0 < n_q; r0 += launch_rows) {
+    const QueryGroup g{w.mask, launch_at(r0)};
+    ws_query_desc d = *qd;
+    if (d.positions) d.positions += 3 * static_cast<int64_t>(r0);
+    AttnPlan p;
+    if (ws_status st = plan_attention(false, static_cast<const uint16_t*>(q) + r0 * q_tok_stride, q_tok_stride,
+                                      q_head_stride, 1, &g, &d, c, static_cast<uint16_t*>(out) + r0 * out_tok_stride,
+                                      out_tok_stride, out_head_stride, stream, &p, &w);
+        st != WS_OK)
+      return st;
+    if (ws_status st = run_plan(c, p, stream); st != WS_OK) return st;
+  }
+  return WS_OK;
 }
 
 // Audio partial rows (fp32 O and log-sum-exp) the static workspace holds next to
@@ -1030,7 +1074,7 @@ ws_status step_attention_impl(ws_cache* c, const ws_attn_call* video, const ws_a
   } else if (ws_status st = timing_mark(c, sa, 1, stream); st != WS_OK) {
     return st;
   }
-  if (pv.few) {  // (8-bit pages: both calls' ranges are the audio merge's)
+  if (pv.few) {  // (its ranges are merged as the audio call's)
     for (const AttnPlan* p : {&pv, &pa})
       if (p->merge)
         if (e = ws::launch_combine(p->cb, stream); e != hipSuccess) return hip_fail(e, "combine launch");
@@ -1074,8 +1118,9 @@ ws_status export_codes(ws_cache* c, const ws::Segment& s, uint8_t* k, uint8_t* v
         for (size_t h = 0; h < H; ++h)
           for (int d = 0; d < ws::kHeadDim; ++d)
             out[((pi * ws::kPageTokens + static_cast<size_t>(slot)) * H + h) * ws::kHeadDim + static_cast<size_t>(d)] =
-                tile[h * ws::kPageHeadElems +
-                     static_cast<size_t>(pool ? ws::v8_tile_index(slot, d) : ws::k8_tile_index(slot, d))];
+                static_cast<uint8_t>(tile[h * ws::kPageHeadElems + static_cast<size_t>(pool ? ws::v8_tile_index(slot, d)
+                                                                                           : ws::k8_tile_index(slot, d))] ^
+                                     (c->format == WS_KV_INT8 ? 0x80 : 0));
     }
   }
   return WS_OK;
@@ -1478,16 +1523,9 @@ ws_status ws_unit_attention_groups(const void* q, int64_t q_tok_stride, int64_t 
 ws_status ws_window_attention(const void* q, int64_t q_tok_stride, int64_t q_head_stride, int32_t n_q,
                               const ws_query_desc* qdesc, ws_cache* cache, const ws_window_spec* window, void* out,
                               int64_t out_tok_stride, int64_t out_head_stride, void* hip_stream) {
-  if (!window) return fail(WS_ERR_INVALID_ARG, "NULL argument");
-  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  const QueryGroup g{ws::MaskSpec{window->mask.q_unit, window->mask.min_visible_unit, window->mask.kind_mask}, n_q};
   try {
-    AttnPlan p;
-    if (ws_status st = plan_attention(false, q, q_tok_stride, q_head_stride, 1, &g, qdesc, cache, out, out_tok_stride,
-                                      out_head_stride, stream, &p, window);
-        st != WS_OK)
-      return st;
-    return run_plan(cache, p, stream);
+    return window_impl(q, q_tok_stride, q_head_stride, n_q, qdesc, cache, window, out, out_tok_stride,
+                       out_head_stride, static_cast<hipStream_t>(hip_stream));
   } catch (...) {
     return fail(WS_ERR_INVALID_ARG, "host allocation failed");
   }

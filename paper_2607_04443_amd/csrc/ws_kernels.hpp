@@ -18,6 +18,8 @@
 
 #include <cstdint>
 
+#include "token_window.hpp"
+
 namespace ws {
 
 constexpr int kHeadDim = 128;
@@ -38,14 +40,14 @@ __host__ __device__ constexpr int v_tile_index(int slot, int d) {
 //   V pool: tile = [128 d][64 slots]
 // so that one 16-byte load is 16 dims of a key, or 16 keys of a dim, and the 16
 // keys (or dims) of an MFMA operand tile cover whole 128-byte lines.
-//   int8: two's complement codes, scale = largest magnitude / 127 in fp32, rounded
+//   int8: bytes code + 128, scale = largest magnitude / 127 in fp32, rounded
 //         up to 16 significant bits: code * scale is exact in fp32, and no code
 //         exceeds 127.
 //   e4m3: scale = the least power of two >= 2^-126 that brings the largest
 //         magnitude to at most 448: a power of two costs a floating-point code
 //         nothing, and code * scale is exact in bf16.
 // The attention takes code * scale rounded to bf16, the type of its matrix
-// operands (and of a bf16 cache's keys).  Empty slots hold code 0.
+// operands (and of a bf16 cache's keys).  Empty slots hold code 0 (int8: byte 128).
 enum KvFormat : int32_t { kFmtBf16 = 0, kFmtInt8 = 1, kFmtE4m3 = 2 };
 __host__ __device__ constexpr int k8_tile_index(int slot, int d) {
   return ((d >> 6) * kPageTokens + slot) * 64 + (d & 63);
@@ -248,19 +250,6 @@ struct GatherArgs {
   uint8_t blk_seg[kMaxPages];
 };
 
-// Token window of an attention call.  The visible tokens under the call's mask,
-// in order, are the timeline; row i of the call sits at index t = t0 + i and sees
-// the keys j with (j > t - window or j < sinks), and j <= t when causal.  The
-// page list then carries each page's first index: entry y = valid | start << 7.
-struct TokenWindow {
-  int32_t on;       // 0: every key of the page list is visible to every row
-  int32_t causal;
-  int32_t t0;
-  int32_t window;   // 1 .. 2^30
-  int32_t sinks;
-  int32_t n_keys;   // tokens of the timeline
-};
-
 // Query class of a video attention call: the rows of one unit's queries in a
 // call that holds queries of several units.  Rows [q0, q0 + n_q) of the call
 // walk entries [page0, page0 + n_pages) of the call's page list (the pages
@@ -269,6 +258,9 @@ struct TokenWindow {
 // pages).  A call with queries of one unit is one class.
 struct AttnClass {
   int32_t q0, n_q, page0, n_pages, n_groups, n_qtiles, wg0, tile_rows;
+  // (token windows) the class's pages are the first head_pages entries from page0
+  // and, after `skip` entries that its rows do not see, the others
+  int32_t head_pages, skip;
   FastDiv by_qtiles;
   VideoPartition32 part;
 };
@@ -379,6 +371,9 @@ hipError_t launch_combine(const CombineArgs& a, hipStream_t stream);
 // per (head, 16-query tile, key range), as the audio path.
 hipError_t launch_kv_append_q(const AppendArgs& a, hipStream_t stream, hipEvent_t start, hipEvent_t stop);
 hipError_t launch_kv_gather(const GatherArgs& a, hipStream_t stream, hipEvent_t start, hipEvent_t stop);
+// Video kernel over 8-bit pages, or under a token window (video_paths.hip); a.win is
+// filled in either case.
+hipError_t launch_path_attention(const AttnArgs& a, hipStream_t stream, hipEvent_t start, hipEvent_t stop);
 hipError_t launch_few_attention(const AttnArgs& a, hipStream_t stream, hipEvent_t start, hipEvent_t stop);
 // The merges of a video call (n_groups > 0) and an audio call (num_heads > 0)
 // in one launch; either may be absent (zero-initialised).
