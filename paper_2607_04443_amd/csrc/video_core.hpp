@@ -1220,6 +1220,12 @@ __device__ __forceinline__ const_class_table class_table() {
       (const __attribute__((address_space(4))) char*)__builtin_amdgcn_kernarg_segment_ptr();
   return (const_class_table)(seg + offsetof(AttnArgs, cls));
 }
+__device__ __forceinline__ ClassPages class_pages(int ci) {
+  const __attribute__((address_space(4))) char* seg =
+      (const __attribute__((address_space(4))) char*)__builtin_amdgcn_kernarg_segment_ptr();
+  const auto* p = (const __attribute__((address_space(4))) ClassPages*)(seg + offsetof(AttnArgs, cls_pages)) + ci;
+  return ClassPages{p->head_pages, p->skip};
+}
 // ------------------------------------------------------------------------- //
 // audio_attn: the few audio queries, memory-bound.  A workgroup of 4 waves
 // takes one (head, 16-query tile, key range); wave w streams pages w, w + 4,
@@ -1637,8 +1643,9 @@ __device__ __forceinline__ void unit_attn(const AttnArgs& a) {
   s.num_heads = a.num_heads;
   if constexpr (P::kWin) {
     s.win = a.win;
-    s.head_pages = tab[ci].head_pages;
-    s.skip = tab[ci].skip;
+    const ClassPages cp = class_pages(ci);
+    s.head_pages = cp.head_pages;
+    s.skip = cp.skip;
     s.hi_all = s.lo_all = 0;  // (a wave without rows asks for no edges)
   }
   if constexpr (P::k8) {

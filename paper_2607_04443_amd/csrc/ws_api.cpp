@@ -553,8 +553,7 @@ void window_classes(const std::vector<ws::PageRef>& list, const ws::TokenWindow&
     cl.q0 = r0;
     cl.n_q = std::min(tile_rows, n_q - r0);
     const ws::WindowPages p = ws::window_range(list, w, r0, cl.n_q);
-    cl.head_pages = p.head;
-    cl.skip = p.skip;
+    a->cls_pages[a->n_classes - 1] = ws::ClassPages{p.head, p.skip};
     cl.n_pages = p.count;
   }
 }
@@ -613,7 +612,7 @@ ws_status plan_attention(bool audio, const void* q, int64_t q_tok_stride, int64_
     cl.page0 = static_cast<int32_t>(c->scratch_list.size());
     if (window) c->pt.window_pages(window->mask, window->win, n_q, &c->scratch_list);
     else c->pt.visible_pages_append(groups[g].mask, &c->scratch_list);
-    cl.head_pages = static_cast<int32_t>(c->scratch_list.size()) - cl.page0;
+    a.cls_pages[n_cls - 1] = ws::ClassPages{static_cast<int32_t>(c->scratch_list.size()) - cl.page0, 0};
     cl.n_pages = static_cast<int32_t>(c->scratch_list.size()) - cl.page0;
   }
   const int32_t n_pages = static_cast<int32_t>(c->scratch_list.size());

@@ -258,13 +258,15 @@ struct GatherArgs {
 // pages).  A call with queries of one unit is one class.
 struct AttnClass {
   int32_t q0, n_q, page0, n_pages, n_groups, n_qtiles, wg0, tile_rows;
-  // (token windows) the class's pages are the first head_pages entries from page0
-  // and, after `skip` entries that its rows do not see, the others
-  int32_t head_pages, skip;
   FastDiv by_qtiles;
   VideoPartition32 part;
 };
 constexpr int kMaxClasses = 8;
+// (token windows) a class's pages are the first head_pages entries from its page0
+// and, after `skip` entries that its rows do not see, the others.
+struct ClassPages {
+  int32_t head_pages, skip;
+};
 
 struct AttnArgs {
   // Visible page lists up to this length travel in the kernel arguments
@@ -329,6 +331,7 @@ struct AttnArgs {
   const float* kscale;   // 8-bit pools: [page][head]
   const float* vscale;
   TokenWindow win;
+  ClassPages cls_pages[kMaxClasses];
   int2 inline_pages[kInlinePages];
 };
 
