@@ -171,7 +171,7 @@ void PageTable::window_pages(const MaskSpec& mask, const TokenWindow& w, int32_t
   out->resize(kept);
 }
 
-WindowPages window_range(const std::vector<PageRef>& list, const TokenWindow& w, int32_t r0, int32_t n_q) {
+ClassPages window_range(const std::vector<PageRef>& list, const TokenWindow& w, int32_t r0, int32_t n_q) {
   const int32_t hi = std::min(w.t0 + r0 + n_q - 1 + w.ahead, w.n_keys), lo = w.t0 + r0 + 1 - w.window;
   auto first_where = [&](auto past) {
     return static_cast<int32_t>(std::partition_point(list.begin(), list.end(), [&](const PageRef& p) {
@@ -183,9 +183,9 @@ WindowPages window_range(const std::vector<PageRef>& list, const TokenWindow& w,
   const int32_t sinks = first_where([&](int32_t start, int32_t) { return start >= sink_hi; });
   const int32_t from = first_where([&](int32_t, int32_t end) { return end > lo; });
   const int32_t to = first_where([&](int32_t start, int32_t) { return start >= hi; });
-  if (from >= to) return WindowPages{sinks, 0, sinks};  // sinks alone
-  if (from <= sinks) return WindowPages{to, 0, to};     // one run
-  return WindowPages{sinks, from - sinks, sinks + to - from};
+  if (from >= to) return ClassPages{sinks, 0, sinks};  // sinks alone
+  if (from <= sinks) return ClassPages{to, 0, to};     // one run
+  return ClassPages{sinks, from - sinks, sinks + to - from};
 }
 
 }  // namespace ws

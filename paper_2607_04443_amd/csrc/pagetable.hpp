@@ -39,12 +39,8 @@ struct MaskSpec {
 
 enum class PtStatus { ok, out_of_pages, unknown, committed, shape };
 
-// The pages of a window call's list that rows r0 .. r0 + n_q - 1 of it see: the
-// first `head` entries and, `skip` entries further, the rest of `count`.
-struct WindowPages {
-  int32_t head, skip, count;
-};
-WindowPages window_range(const std::vector<PageRef>& list, const TokenWindow& w, int32_t r0, int32_t n_q);
+// The pages of a window call's list that rows r0 .. r0 + n_q - 1 of it see.
+ClassPages window_range(const std::vector<PageRef>& list, const TokenWindow& w, int32_t r0, int32_t n_q);
 
 class PageTable {
  public:

@@ -11,6 +11,7 @@
 
 #include <algorithm>
 #include <cstddef>
+#include <type_traits>
 
 #include "quant_device.hpp"
 #include "ws_kernels.hpp"
@@ -419,47 +420,53 @@ struct FewPage {
   u32x4 k[kLoads], v[kLoads];
 };
 
-// Rows and columns past n_valid are read from the zero block (a cache hit).
+// Tiles are read through buffer descriptors: a lane whose row or columns lie past
+// n_valid asks past the end and gets zeros without a memory access.  (Redirected to
+// a block of zeros, such lanes of all CUs meet at its few lines: 2.6 us a page of 4
+// tokens, where a full page takes 1.3.)
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t tile_rsrc(const uint16_t* pool, int64_t tile, int bytes) {
+  const uint64_t at = reinterpret_cast<uint64_t>(pool) + static_cast<uint64_t>(tile) * bytes;
+  return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(at), 0, bytes, 0x00020000);
+}
+constexpr int kPastEnd = 1 << 30;
+template <int kFmt>
+constexpr int kTileBytes = kFmt == kFmtBf16 ? 2 * kPageHeadElems : kPageHeadElems;
+__device__ __forceinline__ u32x4 buffer16(__amdgpu_buffer_rsrc_t r, int lane_off, int off) {
+  return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, lane_off, off, 0));
+}
 template <int kFmt>
 __device__ __forceinline__ void few_load_k(u32x4 (&k)[FewPage<kFmt>::kLoads], const uint16_t* pool, int64_t tile,
-                                           const uint16_t* zeros, int n_valid, int g, int i, int lane) {
+                                           int n_valid, int g, int i) {
+  const auto r = tile_rsrc(pool, tile, kTileBytes<kFmt>);
 #pragma unroll
   for (int t = 0; t < 4; ++t) {
     const int key = key_of<kFmt>(t, i);
-    const bool ok = key < n_valid;
     if constexpr (kFmt == kFmtBf16) {
-      const uint16_t* src = ok ? pool + tile * kPageHeadElems + k_tile_index(key, 8 * g) : zeros + 8 * lane;
-      const int step = ok ? k_tile_index(0, 32) : 0;
+      const int off = key < n_valid ? 2 * k_tile_index(key, 8 * g) : kPastEnd;
 #pragma unroll
-      for (int s = 0; s < 4; ++s) k[4 * t + s] = *reinterpret_cast<const u32x4*>(src + step * s);
+      for (int s = 0; s < 4; ++s) k[4 * t + s] = buffer16(r, off, 2 * k_tile_index(0, 32) * s);
     } else {
-      const uint8_t* src = ok ? reinterpret_cast<const uint8_t*>(pool) + tile * kPageHeadElems + k8_tile_index(key, 16 * g)
-                              : reinterpret_cast<const uint8_t*>(zeros) + 16 * lane;
-      const int step = ok ? k8_tile_index(0, 64) : 0;
+      const int off = key < n_valid ? k8_tile_index(key, 16 * g) : kPastEnd;
 #pragma unroll
-      for (int u = 0; u < 2; ++u) k[2 * t + u] = *reinterpret_cast<const u32x4*>(src + step * u);
+      for (int u = 0; u < 2; ++u) k[2 * t + u] = buffer16(r, off, k8_tile_index(0, 64) * u);
     }
   }
 }
 template <int kFmt>
 __device__ __forceinline__ void few_load_v(u32x4 (&v)[FewPage<kFmt>::kLoads], const uint16_t* pool, int64_t tile,
-                                           const uint16_t* zeros, int n_valid, int g, int i, int lane) {
+                                           int n_valid, int g, int i) {
+  const auto r = tile_rsrc(pool, tile, kTileBytes<kFmt>);
   if constexpr (kFmt == kFmtBf16) {
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
-      const bool ok = 32 * c + 8 * g < n_valid;
-      const uint16_t* src = ok ? pool + tile * kPageHeadElems + v_tile_index(32 * c + 8 * g, i) : zeros + 8 * lane;
-      const int step = ok ? v_tile_index(0, 16) : 0;
+      const int off = 32 * c + 8 * g < n_valid ? 2 * v_tile_index(32 * c + 8 * g, i) : kPastEnd;
 #pragma unroll
-      for (int dt = 0; dt < 8; ++dt) v[2 * dt + c] = *reinterpret_cast<const u32x4*>(src + step * dt);
+      for (int dt = 0; dt < 8; ++dt) v[2 * dt + c] = buffer16(r, off, 2 * v_tile_index(0, 16) * dt);
     }
   } else {
-    const bool ok = 16 * g < n_valid;
-    const uint8_t* src = ok ? reinterpret_cast<const uint8_t*>(pool) + tile * kPageHeadElems + v8_tile_index(16 * g, i)
-                            : reinterpret_cast<const uint8_t*>(zeros) + 16 * lane;
-    const int step = ok ? v8_tile_index(0, 16) : 0;
+    const int off = 16 * g < n_valid ? v8_tile_index(16 * g, i) : kPastEnd;
 #pragma unroll
-    for (int dt = 0; dt < 8; ++dt) v[dt] = *reinterpret_cast<const u32x4*>(src + step * dt);
+    for (int dt = 0; dt < 8; ++dt) v[dt] = buffer16(r, off, v8_tile_index(0, 16) * dt);
   }
 }
 __device__ __forceinline__ bf16x8 operand(u32x4 w) { return __builtin_bit_cast(bf16x8, w); }
@@ -483,6 +490,8 @@ __device__ __forceinline__ const_page_list call_pages(const AttnArgs& a) {
   return (const_page_list)(seg + offsetof(AttnArgs, inline_pages));
 }
 
+typedef const __attribute__((address_space(4))) float* const_floats;
+
 template <int kFmt>
 __global__ __launch_bounds__(256, 2) void few_attn_kernel(const AttnArgs a) {
   __shared__ float sm_o[4][kHeadDim][16];  // per wave O^T, merged at the end
@@ -500,22 +509,30 @@ __global__ __launch_bounds__(256, 2) void few_attn_kernel(const AttnArgs a) {
   const const_page_list pages = call_pages(a);
   const bool window = a.win.on != 0;
 
+  // (the scales come with a page's entry, a page ahead of their use)
   struct Entry {
     int valid, start;
     int64_t tile;
+    float ks, vs;
   };
+  const const_floats kscale = (const_floats)a.kscale, vscale = (const_floats)a.vscale;
   auto entry = [&](int p) {
-    if (p >= p_end) return Entry{0, 0, 0};  // past the last page: zeros
+    if (p >= p_end) return Entry{0, 0, 0, 1.f, 1.f};  // past the last page: zeros
     const int x = pages[p].x;
     const uint32_t y = static_cast<uint32_t>(pages[p].y);
-    return Entry{static_cast<int>(y & 127u), static_cast<int>(y >> 7), static_cast<int64_t>(x) * a.num_heads + head};
+    Entry e{static_cast<int>(y & 127u), static_cast<int>(y >> 7), static_cast<int64_t>(x) * a.num_heads + head, 1.f, 1.f};
+    if (kFmt != kFmtBf16) {
+      e.ks = kscale[e.tile];
+      e.vs = vscale[e.tile];
+    }
+    return e;
   };
 
   // the wave's first page is requested before the query prologue
   FewPage<kFmt> pg;
   Entry cur = entry(p_begin);
-  few_load_k<kFmt>(pg.k, a.kpool, cur.tile, a.zeros, cur.valid, g, i16, lane);
-  few_load_v<kFmt>(pg.v, a.vpool, cur.tile, a.zeros, cur.valid, g, i16, lane);
+  few_load_k<kFmt>(pg.k, a.kpool, cur.tile, cur.valid, g, i16);
+  few_load_v<kFmt>(pg.v, a.vpool, cur.tile, cur.valid, g, i16);
 
   // lane holds Q''[q][dims_of(s, g) ..], with the softmax scale and log2(e) in it
   const int q = qtile * kAudioQTile + i16;
@@ -583,19 +600,21 @@ __global__ __launch_bounds__(256, 2) void few_attn_kernel(const AttnArgs a) {
   f32x4 o[8];
 #pragma unroll
   for (int dt = 0; dt < 8; ++dt) o[dt] = (f32x4){0.f, 0.f, 0.f, 0.f};
-  for (int p = p_begin; p < p_end; p += 4) {
-    const QuantScale ks = quant_scale<kFmt>(kFmt == kFmtBf16 ? 1.f : a.kscale[cur.tile]);
-    const QuantScale vs = quant_scale<kFmt>(kFmt == kFmtBf16 ? 1.f : a.vscale[cur.tile]);
+  // one page: the first kChunks of the two 32-key chunks (8-bit pages of up to 8
+  // tokens, such as a unit's audio, have keys in the first alone)
+  auto attend = [&](auto chunks, int p) __attribute__((always_inline)) {
+    constexpr int kChunks = decltype(chunks)::value;
+    const QuantScale ks = quant_scale<kFmt>(cur.ks), vs = quant_scale<kFmt>(cur.vs);
     const Entry nxt = entry(p + 4);
-    f32x4 sacc[4];
+    f32x4 sacc[2 * kChunks];
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
+    for (int t = 0; t < 2 * kChunks; ++t) {
       sacc[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int s = 0; s < 4; ++s)
         sacc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k_operand<kFmt>(pg.k, t, s, ks), qreg[s], sacc[t], 0, 0, 0);
     }
-    few_load_k<kFmt>(pg.k, a.kpool, nxt.tile, a.zeros, nxt.valid, g, i16, lane);
+    few_load_k<kFmt>(pg.k, a.kpool, nxt.tile, nxt.valid, g, i16);
     const bool whole = cur.valid == kPageTokens &&
                        (!window || (cur.start + kPageTokens <= hi_all &&
                                     (cur.start >= lo_all || cur.start + kPageTokens <= a.win.sinks)));
@@ -603,7 +622,7 @@ __global__ __launch_bounds__(256, 2) void few_attn_kernel(const AttnArgs a) {
       const int hi = window ? min(cur.valid, row.hi - cur.start) : cur.valid;
       const int lo = window ? row.lo - cur.start : 0, sk = window ? a.win.sinks - cur.start : 0;
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
+      for (int t = 0; t < 2 * kChunks; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int slot = key_of<kFmt>(t, 4 * g + r);
@@ -613,7 +632,7 @@ __global__ __launch_bounds__(256, 2) void few_attn_kernel(const AttnArgs a) {
     if (!fixed_shift) {
       float mx = kNegInf;
 #pragma unroll
-      for (int t = 0; t < 4; ++t) mx = fmaxf(mx, fmaxf(fmaxf(sacc[t][0], sacc[t][1]), fmaxf(sacc[t][2], sacc[t][3])));
+      for (int t = 0; t < 2 * kChunks; ++t) mx = fmaxf(mx, fmaxf(fmaxf(sacc[t][0], sacc[t][1]), fmaxf(sacc[t][2], sacc[t][3])));
       mx = pair_max<32>(pair_max<16>(mx));
       const float m_new = fmaxf(m_run, mx);
       const float alpha = m_new == kNegInf ? 1.f : fast_exp2(m_run - m_new);
@@ -623,10 +642,10 @@ __global__ __launch_bounds__(256, 2) void few_attn_kernel(const AttnArgs a) {
       for (int dt = 0; dt < 8; ++dt) o[dt] *= alpha;
     }
     const float m_use = m_run == kNegInf ? 0.f : m_run;
-    u32x4 pw[2];
+    u32x4 pw[kChunks];
     const bf16x2 ones = {static_cast<__bf16>(1.0f), static_cast<__bf16>(1.0f)};
 #pragma unroll
-    for (int c = 0; c < 2; ++c)
+    for (int c = 0; c < kChunks; ++c)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const f32x4& sc = sacc[2 * c + h];
@@ -638,12 +657,16 @@ __global__ __launch_bounds__(256, 2) void few_attn_kernel(const AttnArgs a) {
         l_run = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w1), ones, l_run, false);
       }
 #pragma unroll
-    for (int c = 0; c < 2; ++c)
+    for (int c = 0; c < kChunks; ++c)
 #pragma unroll
       for (int dt = 0; dt < 8; ++dt)
         o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v_operand<kFmt>(pg.v, dt, c, vs), operand(pw[c]), o[dt], 0, 0, 0);
-    few_load_v<kFmt>(pg.v, a.vpool, nxt.tile, a.zeros, nxt.valid, g, i16, lane);
+    few_load_v<kFmt>(pg.v, a.vpool, nxt.tile, nxt.valid, g, i16);
     cur = nxt;
+  };
+  for (int p = p_begin; p < p_end; p += 4) {
+    if (kFmt != kFmtBf16 && cur.valid <= 8) attend(std::integral_constant<int, 1>{}, p);
+    else attend(std::integral_constant<int, 2>{}, p);
   }
 
   // merge the four waves: lane holds O^T[16 dt + 4 g + r][q] of its keys

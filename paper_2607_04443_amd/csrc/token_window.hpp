@@ -20,4 +20,10 @@ struct TokenWindow {
 constexpr int32_t kMaxTimeline = 1 << 24;  // tokens that page entries can index
 constexpr int32_t kNoWindow = 1 << 30;     // (a timeline and 2^20 rows past it stay below 2^31 with it)
 
+// The pages of a query class, or of a query tile, within a window call's list: its
+// first head_pages entries and, `skip` entries further, the others of `count`.
+struct ClassPages {
+  int32_t head_pages, skip, count;
+};
+
 }  // namespace ws

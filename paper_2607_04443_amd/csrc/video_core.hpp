@@ -204,6 +204,7 @@ struct Stream8 {
 struct StreamWin {
   int start[2];          // first timeline index of the window's units
   int head_pages, skip;  // the class's list: head_pages pages, then after `skip` others the rest
+  int head0;             // head of stream index 0 (launches without classes)
   int hi_all, lo_all;    // keys [lo_all, hi_all) are seen by every row of the wave
   TokenWindow win;
 };
@@ -237,6 +238,11 @@ __device__ __forceinline__ int stream_place(const VideoStream<P>& s, int at) {
   if constexpr (P::kWin) at += at >= s.head_pages ? s.skip : 0;
   return s.page0 + at;
 }
+template <class P>
+__device__ __forceinline__ uint32_t head_of(const VideoStream<P>& s, uint32_t head) {
+  if constexpr (P::kWin) head += s.head0;
+  return head;
+}
 // A list entry's valid tokens; with a window its first timeline index.
 template <class P>
 __device__ __forceinline__ uint32_t valid_of(int y) {
@@ -249,7 +255,7 @@ __device__ __forceinline__ uint32_t stream_entry(const VideoStream<P>& s, int k,
   const int pi = stream_place(s, static_cast<int>(x - head * s.n_pages));
   const int y = s.pages[pi].y;
   if (start) *start = start_of(y);
-  return ((s.pages[pi].x * s.num_heads + head) << 7) | valid_of<P>(y);
+  return ((s.pages[pi].x * s.num_heads + head_of(s, head)) << 7) | valid_of<P>(y);
 }
 // The first window: its list entries requested, then combined.
 template <class P>
@@ -258,7 +264,7 @@ __device__ __forceinline__ void stream_request(VideoStream<P>& s) {
   for (int k = 0; k < 2; ++k) {
     const uint32_t x = s.lo + min(64 * k + s.lane, s.n - 1), head = fast_div(x, s.div_pages);
     const int pi = stream_place(s, static_cast<int>(x - head * s.n_pages));
-    s.raw_head[k] = head;
+    s.raw_head[k] = head_of(s, head);
     s.raw_page[k] = s.pages[pi].x;
     s.raw_valid[k] = s.pages[pi].y;
   }
@@ -1158,7 +1164,7 @@ __device__ __forceinline__ void video_segment(const AttnArgs& a, const VideoSeg&
           a, sg.head, wrow, min(16 * kQT, sg.q_hi - wrow), 0, sg.n, 1, lane_e,
           [&](int p) {
             const uint32_t x = s.lo + first + p;
-            const int pi = stream_place(s, static_cast<int>(x - sg.head * s.n_pages));
+            const int pi = stream_place(s, static_cast<int>(x - (sg.head - s.head0) * s.n_pages));
             return make_int2(s.pages[pi].x, s.pages[pi].y);
           },
           [&](int i, float m, float l, float o0, float o1) {
@@ -1224,7 +1230,7 @@ __device__ __forceinline__ ClassPages class_pages(int ci) {
   const __attribute__((address_space(4))) char* seg =
       (const __attribute__((address_space(4))) char*)__builtin_amdgcn_kernarg_segment_ptr();
   const auto* p = (const __attribute__((address_space(4))) ClassPages*)(seg + offsetof(AttnArgs, cls_pages)) + ci;
-  return ClassPages{p->head_pages, p->skip};
+  return ClassPages{p->head_pages, p->skip, p->count};
 }
 // ------------------------------------------------------------------------- //
 // audio_attn: the few audio queries, memory-bound.  A workgroup of 4 waves
@@ -1559,7 +1565,7 @@ __device__ __forceinline__ VideoSeg video_seg(const VideoWork& w, const VideoStr
   const int head = static_cast<int>(fast_div(x, s.div_pages)), h0 = head * s.n_pages;
   const int n = min(s.n - k, h0 + s.n_pages - x);
   const int seg = x == h0 ? 0 : w.group - static_cast<int>(part_group_of(w.part, h0));
-  return VideoSeg{head, n, seg, w.q_lo, w.q_hi, x == h0 && n == s.n_pages};
+  return VideoSeg{static_cast<int>(head_of(s, head)), n, seg, w.q_lo, w.q_hi, x == h0 && n == s.n_pages};
 }
 
 // Ranges of a head (for the rider rows' partials).
@@ -1627,8 +1633,20 @@ __device__ __forceinline__ void unit_attn(const AttnArgs& a) {
   const int n_qtiles = tab[ci].n_qtiles;
   const int group = static_cast<int>(fast_div(local, FastDiv{tab[ci].by_qtiles.mul, tab[ci].by_qtiles.shift}));
   const int qt = local - group * n_qtiles;
-  const int q0 = tab[ci].q0, q_hi = q0 + tab[ci].n_q;
-  const int tile_rows = tab[ci].tile_rows, q_lo = q0 + qt * tile_rows;
+  int q0 = tab[ci].q0, q_hi = q0 + tab[ci].n_q;
+  int tile_rows = tab[ci].tile_rows, q_lo = q0 + qt * tile_rows;
+  [[maybe_unused]] int head0 = 0;
+  [[maybe_unused]] bool tiles = false;
+  if constexpr (P::kWin) {
+    if (a.n_tiles > 0) {
+      tiles = true;
+      head0 = static_cast<int>(fast_div(item, a.by_tiles));
+      ci = item - head0 * a.n_tiles;
+      tile_rows = a.tile_rows;
+      q_lo = ci * tile_rows;
+      q_hi = min(q_lo + tile_rows, a.n_q);
+    }
+  }
   // rider rows follow the video rows (a single class then)
   const int row_end = min(q_lo + tile_rows, P::kPlain && a.n_rq > 0 ? a.rq_row0 + a.n_rq : q_hi);
   const int wave_rows = video_wave_rows(tile_rows, row_end - q_lo);
@@ -1646,14 +1664,19 @@ __device__ __forceinline__ void unit_attn(const AttnArgs& a) {
     const ClassPages cp = class_pages(ci);
     s.head_pages = cp.head_pages;
     s.skip = cp.skip;
+    s.head0 = head0;
+    s.n_pages = cp.count;
+    s.page0 = tiles ? 0 : tab[ci].page0;
     s.hi_all = s.lo_all = 0;  // (a wave without rows asks for no edges)
   }
   if constexpr (P::k8) {
     s.kscale = a.kscale;
     s.vscale = a.vscale;
   }
-  s.n_pages = tab[ci].n_pages;
-  s.page0 = tab[ci].page0;
+  if constexpr (!P::kWin) {
+    s.n_pages = tab[ci].n_pages;
+    s.page0 = tab[ci].page0;
+  }
   s.lane = lane;
   s.kpool = a.kpool;
   s.vpool = a.vpool;
@@ -1661,13 +1684,21 @@ __device__ __forceinline__ void unit_attn(const AttnArgs& a) {
   s.stage = 0;
   s.valid = 0;
   if (s.n_pages == 0) {  // nothing visible: one group per head
-    if (group < a.num_heads) video_empty(a, group, q_lo, min(q_lo + tile_rows, q_hi));
+    const int head = tiles ? head0 : group;
+    if (head < a.num_heads) video_empty(a, head, q_lo, min(q_lo + tile_rows, q_hi));
     return;
   }
   w.part = part_of(tab[ci]);
   s.div_pages = w.part.by_pages;
   s.lo = static_cast<int>(part_group_lo(w.part, group));
   s.n = static_cast<int>(part_group_lo(w.part, group + 1)) - s.lo;
+  if constexpr (P::kWin) {
+    if (tiles) {
+      s.div_pages = FastDiv{1, 0};  // (quotient 0)
+      s.lo = 0;
+      s.n = s.n_pages;
+    }
+  }
   if (s.n == 0) return;
   // the list entries of the window are under way while the lane's offsets are
   // computed; stream_start waits for them, and the first segment's queries are

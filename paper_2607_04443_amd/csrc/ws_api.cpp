@@ -518,6 +518,7 @@ struct WindowCall {
   ws::MaskSpec mask;
   ws::TokenWindow win;
   int32_t tile_rows;  // of the video kernel's form
+  bool whole_heads;   // a workgroup takes a tile of a head over all its pages (no classes)
 };
 
 // Checks a window and resolves it against the cache.
@@ -552,8 +553,8 @@ void window_classes(const std::vector<ws::PageRef>& list, const ws::TokenWindow&
     cl = ws::AttnClass{};
     cl.q0 = r0;
     cl.n_q = std::min(tile_rows, n_q - r0);
-    const ws::WindowPages p = ws::window_range(list, w, r0, cl.n_q);
-    a->cls_pages[a->n_classes - 1] = ws::ClassPages{p.head, p.skip};
+    const ws::ClassPages p = ws::window_range(list, w, r0, cl.n_q);
+    a->cls_pages[a->n_classes - 1] = p;
     cl.n_pages = p.count;
   }
 }
@@ -612,8 +613,8 @@ ws_status plan_attention(bool audio, const void* q, int64_t q_tok_stride, int64_
     cl.page0 = static_cast<int32_t>(c->scratch_list.size());
     if (window) c->pt.window_pages(window->mask, window->win, n_q, &c->scratch_list);
     else c->pt.visible_pages_append(groups[g].mask, &c->scratch_list);
-    a.cls_pages[n_cls - 1] = ws::ClassPages{static_cast<int32_t>(c->scratch_list.size()) - cl.page0, 0};
     cl.n_pages = static_cast<int32_t>(c->scratch_list.size()) - cl.page0;
+    a.cls_pages[n_cls - 1] = ws::ClassPages{cl.n_pages, 0, cl.n_pages};
   }
   const int32_t n_pages = static_cast<int32_t>(c->scratch_list.size());
   if (n_pages <= ws::AttnArgs::kInlinePages) {
@@ -626,7 +627,7 @@ ws_status plan_attention(bool audio, const void* q, int64_t q_tok_stride, int64_
     if (ws_status st = arena_list(c, masks, n_cls, a.win, window ? n_q : 0, stream, &plist); st != WS_OK) return st;
   }
   a.n_classes = n_cls;
-  if (window && plan->path) {
+  if (window && plan->path && !window->whole_heads) {
     window_classes(c->scratch_list, a.win, n_q, window->tile_rows, &a);
     n_cls = a.n_classes;
   }
@@ -663,7 +664,18 @@ ws_status plan_attention(bool audio, const void* q, int64_t q_tok_stride, int64_
   const int64_t cap = c->part_rows / (static_cast<int64_t>(H) * n_q);
   int splits = 1;         // audio: key ranges; video: workgroup groups
   bool merge = few_rows;
-  if (few_rows) {
+  if (window && plan->path && window->whole_heads) {
+    a.n_classes = 0;
+    a.n_tiles = (n_q + window->tile_rows - 1) / window->tile_rows;
+    a.tile_rows = window->tile_rows;
+    a.by_tiles = ws::make_fast_div(static_cast<uint32_t>(a.n_tiles));
+    for (int t = 0; t < a.n_tiles; ++t)
+      a.cls_pages[t] = ws::window_range(c->scratch_list, a.win, t * a.tile_rows,
+                                        std::min(a.tile_rows, n_q - t * a.tile_rows));
+    a.n_wg = a.n_tiles * H;
+    a.n_splits = 1;
+    splits = a.n_wg;
+  } else if (few_rows) {
     splits = choose_audio_splits(c, n_items, n_pages);
     splits = std::max(1, std::min(splits, std::max(1, n_pages)));
     splits = static_cast<int>(std::min<int64_t>(splits, std::max<int64_t>(cap, 1)));
@@ -803,6 +815,42 @@ ws_status attention_impl(bool audio, const void* q, int64_t q_tok_stride, int64_
   return run_plan(c, p, stream);
 }
 
+// Tiles of a window call in the video kernel's form, by an estimate in us from the
+// same measurements as video_tiling: tiles of 256, 192 or 128 rows as classes that
+// share out their pages over one round of the CUs, eight to a launch, merged where
+// heads are split; or a workgroup for each tile of each head.
+void window_tiling(ws_cache* c, int32_t n_q, WindowCall* w) {
+  w->tile_rows = ws::kVideoQTile;
+  w->whole_heads = false;
+  if (c->opt_video_splits > 0) return;  // (forced ranges keep the full tile)
+  const double H = c->cfg.num_heads, cus = c->num_cus;
+  double best = -1.0;
+  for (int rows : {256, 192, 128}) {
+    const int32_t tiles = (n_q + rows - 1) / rows, mid = tiles / 2 * rows;
+    const int wave_rows = ws::video_wave_rows(rows, std::min(rows, n_q));
+    ws::TokenWindow t = w->win;  // a tile in the middle of the call
+    t.t0 += mid;
+    c->scratch_list.clear();
+    c->pt.window_pages(w->mask, t, std::min(rows, n_q - mid), &c->scratch_list);
+    const double pages = std::max<double>(1.0, static_cast<double>(c->scratch_list.size()));
+    const double first = ws::video_first_us(wave_rows);
+    // a round of workgroups lasts as long as one of them; from three on they even out
+    const double wgs = tiles * H / cus, rounds = wgs < 3.0 ? std::ceil(wgs) : wgs + 0.5;
+    const double whole_us = rounds * (first + pages * ws::video_page_us(wave_rows, std::min(1.0, wgs)));
+    const double units = std::min<int32_t>(tiles, ws::kMaxClasses) * H * pages, groups = std::min(cus, units);
+    const double launches = (tiles + ws::kMaxClasses - 1) / ws::kMaxClasses, share = units / groups;
+    const double split_us =
+        launches * (first + share * ws::video_page_us(wave_rows, groups / cus) + 5.0 * share / pages + 9.0);
+    for (bool whole : {false, true}) {
+      const double us = whole ? whole_us : split_us;
+      if (best >= 0.0 && us >= best) continue;
+      best = us;
+      w->tile_rows = rows;
+      w->whole_heads = whole;
+    }
+  }
+}
+
 // A window call: few rows at once, or the video kernel's form in launches of up to
 // kMaxClasses query tiles, each over the pages that its rows see.
 ws_status window_impl(const void* q, int64_t q_tok_stride, int64_t q_head_stride, int32_t n_q, const ws_query_desc* qd,
@@ -818,13 +866,8 @@ ws_status window_impl(const void* q, int64_t q_tok_stride, int64_t q_head_stride
   if (ws_status st = resolve_window(c, *spec, n_q, &w); st != WS_OK) return st;
   int32_t launch_rows = n_q;
   if (n_q > kFewRows) {
-    w.tile_rows = ws::kVideoQTile;
-    if (c->opt_video_splits == 0) {
-      c->scratch_list.clear();
-      c->pt.window_pages(w.mask, w.win, std::min(n_q, ws::kVideoQTile), &c->scratch_list);
-      w.tile_rows = ws::video_tiling(H, n_q, static_cast<int64_t>(c->scratch_list.size()), c->num_cus).rows;
-    }
-    launch_rows = ws::kMaxClasses * w.tile_rows;
+    window_tiling(c, n_q, &w);
+    launch_rows = (w.whole_heads ? ws::kMaxTiles : ws::kMaxClasses) * w.tile_rows;
   }
   const int32_t t0 = w.win.t0;
   auto launch_at = [&](int32_t r0) {

@@ -262,11 +262,7 @@ struct AttnClass {
   VideoPartition32 part;
 };
 constexpr int kMaxClasses = 8;
-// (token windows) a class's pages are the first head_pages entries from its page0
-// and, after `skip` entries that its rows do not see, the others.
-struct ClassPages {
-  int32_t head_pages, skip;
-};
+constexpr int kMaxTiles = 64;  // query tiles of a window launch without classes
 
 struct AttnArgs {
   // Visible page lists up to this length travel in the kernel arguments
@@ -331,7 +327,14 @@ struct AttnArgs {
   const float* kscale;   // 8-bit pools: [page][head]
   const float* vscale;
   TokenWindow win;
-  ClassPages cls_pages[kMaxClasses];
+  // Window launches with n_tiles > 0 have no classes: tile k holds rows tile_rows k
+  // .. of the call, one workgroup takes one tile of one head over all of the tile's
+  // pages (item = head * n_tiles + tile), and nothing is merged.  cls_pages: of the
+  // classes, or of the tiles.
+  int32_t n_tiles;
+  int32_t tile_rows;
+  FastDiv by_tiles;
+  ClassPages cls_pages[kMaxTiles];
   int2 inline_pages[kInlinePages];
 };
 
@@ -484,6 +487,11 @@ struct VideoTiling {
   int rows;        // per query tile
   int64_t groups;  // video_group_count of that tiling
 };
+// A page, and a launch with its first segment, by the wave's rows (load: the CUs at work).
+inline double video_page_us(int wave_rows, double load) {
+  return (wave_rows == 64 ? 1.0 : wave_rows == 48 ? 0.83 : 0.6) * (0.49 + 0.96 * load);
+}
+inline double video_first_us(int wave_rows) { return wave_rows == 64 ? 14.5 : wave_rows == 48 ? 13.3 : 11.5; }
 inline double video_tiling_us(int64_t heads, int64_t n_q, int64_t pages, int64_t cus, const VideoTiling& t) {
   const int64_t g = t.groups, qtiles = (n_q + t.rows - 1) / t.rows;
   const int64_t one_round = cus / qtiles > 1 ? cus / qtiles : 1;
@@ -492,8 +500,7 @@ inline double video_tiling_us(int64_t heads, int64_t n_q, int64_t pages, int64_t
   const double segs = static_cast<double>(!split || g % heads == 0 ? (g > heads ? g : heads) : g + heads - 1) / g;
   const double load = g * qtiles < cus ? static_cast<double>(g * qtiles) / cus : 1.0;
   const int wave_rows = video_wave_rows(t.rows, static_cast<int>(n_q < t.rows ? n_q : t.rows));
-  const double page = (wave_rows == 64 ? 1.0 : wave_rows == 48 ? 0.83 : 0.6) * (0.49 + 0.96 * load);
-  const double first = wave_rows == 64 ? 14.5 : wave_rows == 48 ? 13.3 : 11.5;
+  const double page = video_page_us(wave_rows, load), first = video_first_us(wave_rows);
   const int last = static_cast<int>(n_q - (qtiles - 1) * t.rows) + kAudioQTile;
   const double audio = last > t.rows ? 5.0 : last > (kVideoWaves - 1) * video_wave_rows(t.rows, last) ? 1.0 : 0.0;
   return rounds * (static_cast<double>(heads * pages) / g * page + first + 5.0 * (segs - 1.0)) + (split ? 6.0 : 0.0) + audio;
