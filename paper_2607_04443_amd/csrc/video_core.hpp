@@ -174,7 +174,7 @@ struct Ctx8 {
 };
 struct CtxWin {
   int start;               // the page's first timeline index
-  int edge;                // some row of the wave does not see all 64 slots
+  int edge;                // what hides slots of it from rows of the wave (kEdge*)
 };
 template <class P>
 struct PageCtx : std::conditional_t<P::k8, Ctx8, Nothing<0>>, std::conditional_t<P::kWin, CtxWin, Nothing<1>> {
@@ -433,12 +433,17 @@ __device__ __forceinline__ void set_reads(const VideoStream<P>& s, uint32_t stag
   c.vp = (s.v_read + ring_add(stage, kStages - 1)) ^ 64u;
 }
 
-// Whether some row of the wave does not see all of a page.
+// What hides slots of a page from some row of the wave: its end (the page's valid
+// tokens, or a row's last key), and a row's first key, in a page with sinks or
+// without.  (Each a pass of its own over the S tiles, two or three instructions a
+// value: all three conditions at once take five.)
+constexpr int kEdgeHi = 1, kEdgeLo = 2, kEdgeSinks = 4;
 template <class P>
 __device__ __forceinline__ int page_edge(const VideoStream<P>& s, int start, int valid) {
   const int end = start + kPageTokens;
-  const int e = (valid < kPageTokens) | (end > s.hi_all) | ((start < s.lo_all) & (end > s.win.sinks));
-  return __builtin_amdgcn_readfirstlane(e);
+  const int lo = (start < s.lo_all) & (end > s.win.sinks) ? (start < s.win.sinks ? kEdgeSinks : kEdgeLo) : 0;
+  const int hi = (valid < kPageTokens) | (end > s.hi_all) ? kEdgeHi : 0;
+  return __builtin_amdgcn_readfirstlane(lo | hi);
 }
 
 // Starts the stream: key norms of its first window, the loads of its first
@@ -721,19 +726,25 @@ __device__ __forceinline__ void video_iter(VideoState<kQT>& st, VideoStream<P>& 
       const int lim = n_valid - off;
       if constexpr (P::kWin) {
         // row by row: keys at or past hi, and from the sinks' end up to lo, are hidden
+        const int at = c.start + off;
+        auto hide = [&](auto&& hidden) __attribute__((always_inline)) {
 #pragma unroll
-        for (int j = 0; j < kQT; ++j) {
-          const RowRange rr = row_range(s.win, st.t_row + 16 * j);
-          const int hi = min(lim, rr.hi - c.start - off), sk = s.win.sinks - c.start - off;
-          const uint32_t hidden = max(rr.lo - s.win.sinks, 0);
+          for (int j = 0; j < kQT; ++j) {
+            const RowRange rr = row_range(s.win, st.t_row + 16 * j);
 #pragma unroll
-          for (int t = a; t < a + 2; ++t)
+            for (int t = a; t < a + 2; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const int slot = 32 * (t >> 1) + 4 * (t & 1) + r;
-              const bool hide = (slot >= hi) | (static_cast<uint32_t>(slot - sk) < hidden);
-              sa[t][j][r] = hide ? kNegInf : sa[t][j][r];
-            }
+              for (int r = 0; r < 4; ++r)
+                sa[t][j][r] = hidden(rr, 32 * (t >> 1) + 4 * (t & 1) + r) ? kNegInf : sa[t][j][r];
+          }
+        };
+        if (c.edge & kEdgeHi)
+          hide([&](const RowRange& rr, int slot) __attribute__((always_inline)) { return slot >= min(lim, rr.hi - at); });
+        if (c.edge & kEdgeLo)
+          hide([&](const RowRange& rr, int slot) __attribute__((always_inline)) { return slot < rr.lo - at; });
+        if (c.edge & kEdgeSinks) {
+          const int sk = s.win.sinks - at;
+          hide([&](const RowRange& rr, int slot) __attribute__((always_inline)) { return slot >= sk && slot < rr.lo - at; });
         }
       } else {
 #pragma unroll
