@@ -508,16 +508,29 @@ ws_status refuse_capture(hipStream_t stream) {
   return WS_OK;
 }
 
-// Rows of a unit attention (8-bit pages) or a window attention that go to the
-// kernel of few rows.
-constexpr int kFewRows = 64;
+// What a call takes in the kernel of few rows, in us, for a unit attention over 8-bit
+// pages or a window attention; the video kernel's form takes it over where its own
+// estimate is lower.  Each 16-row tile of a head walks all pages of the call's list on
+// its own; past 12 of them the ranges are merged.  Measured, few rows / video form:
+//   e4m3, 40 heads,   8 pages:  64 rows  9 / 16,  256  17 / 22,  512  27 / 21
+//   e4m3, 40 heads, 128 pages:  16 rows 23 / 36,   32  33 / 37,   64  57 / 39
+//   int8, 12 heads,  32 pages:  64 rows 15 / 21,  256  24 / 25,  512  32 / 28
+//   int8,  4 heads, 128 pages: 128 rows 20 / 38,  256  26 / 43,  512  39 / 45
+//   bf16, 40 heads, window of 1024: 64 rows 23 / 24,  128  36 / 27
+double few_rows_us(const ws_cache* c, int32_t n_q, int32_t n_pages) {
+  const double units = static_cast<double>(c->cfg.num_heads) * ((n_q + ws::kAudioQTile - 1) / ws::kAudioQTile) * n_pages;
+  return 8.0 + (n_pages > kAudioDirectPages ? 4.5 : 0.0) + (c->format == WS_KV_BF16 ? 0.0035 : 0.0025) * units;
+}
+
+constexpr int32_t kFewRowsAtMost = 4096;  // (a window's list is that of all its rows)
 
 // A window call's own part: the segments of its timeline, and the rows' window
 // (t0: of the call's first row).
 struct WindowCall {
   ws::MaskSpec mask;
   ws::TokenWindow win;
-  int32_t tile_rows;  // of the video kernel's form
+  bool few;           // the kernel of few rows; else the video kernel's form:
+  int32_t tile_rows;
   bool whole_heads;   // a workgroup takes a tile of a head over all its pages (no classes)
 };
 
@@ -594,9 +607,6 @@ ws_status plan_attention(bool audio, const void* q, int64_t q_tok_stride, int64_
   // distinct list).
   plan->audio = audio;
   const bool special = window || c->format != WS_KV_BF16;
-  plan->few = special && (audio || (n_groups == 1 && n_q <= kFewRows));
-  plan->path = special && !plan->few;
-  const bool few_rows = audio || plan->few;  // key ranges of 16-row tiles, merged in fp32
   ws::AttnArgs& a = plan->a;
   a = ws::AttnArgs{};
   a.win = window ? window->win : ws::TokenWindow{0, ws::kNoWindow, 0, ws::kNoWindow, 0, ws::kNoWindow};
@@ -617,6 +627,14 @@ ws_status plan_attention(bool audio, const void* q, int64_t q_tok_stride, int64_
     a.cls_pages[n_cls - 1] = ws::ClassPages{cl.n_pages, 0, cl.n_pages};
   }
   const int32_t n_pages = static_cast<int32_t>(c->scratch_list.size());
+  if (window) plan->few = window->few;
+  else if (special && !audio && n_groups == 1 && c->opt_video_splits == 0)
+    plan->few = n_pages == 0 || few_rows_us(c, n_q, n_pages) <=
+                                    ws::video_tiling_us(H, n_q, n_pages, c->num_cus,
+                                                        ws::video_tiling(H, n_q, n_pages, c->num_cus));
+  else plan->few = special && audio;
+  plan->path = special && !plan->few;
+  const bool few_rows = audio || plan->few;  // key ranges of 16-row tiles, merged in fp32
   if (n_pages <= ws::AttnArgs::kInlinePages) {
     for (int32_t i = 0; i < n_pages; ++i)
       a.inline_pages[i] = make_int2(c->scratch_list[static_cast<size_t>(i)].page,
@@ -820,9 +838,16 @@ ws_status attention_impl(bool audio, const void* q, int64_t q_tok_stride, int64_
 // share out their pages over one round of the CUs, eight to a launch, merged where
 // heads are split; or a workgroup for each tile of each head.
 void window_tiling(ws_cache* c, int32_t n_q, WindowCall* w) {
+  w->few = false;
   w->tile_rows = ws::kVideoQTile;
   w->whole_heads = false;
   if (c->opt_video_splits > 0) return;  // (forced ranges keep the full tile)
+  if (n_q <= kFewRowsAtMost) {
+    c->scratch_list.clear();
+    c->pt.window_pages(w->mask, w->win, n_q, &c->scratch_list);
+    w->few = true;
+  }
+  const double few_us = w->few ? few_rows_us(c, n_q, static_cast<int32_t>(c->scratch_list.size())) : -1.0;
   const double H = c->cfg.num_heads, cus = c->num_cus;
   double best = -1.0;
   for (int rows : {256, 192, 128}) {
@@ -849,6 +874,7 @@ void window_tiling(ws_cache* c, int32_t n_q, WindowCall* w) {
       w->whole_heads = whole;
     }
   }
+  w->few = w->few && few_us <= best;
 }
 
 // A window call: few rows at once, or the video kernel's form in launches of up to
@@ -864,11 +890,8 @@ ws_status window_impl(const void* q, int64_t q_tok_stride, int64_t q_head_stride
   if (ws_status st = check_strides("out", out, out_tok_stride, out_head_stride, n_q, H); st != WS_OK) return st;
   WindowCall w{};
   if (ws_status st = resolve_window(c, *spec, n_q, &w); st != WS_OK) return st;
-  int32_t launch_rows = n_q;
-  if (n_q > kFewRows) {
-    window_tiling(c, n_q, &w);
-    launch_rows = (w.whole_heads ? ws::kMaxTiles : ws::kMaxClasses) * w.tile_rows;
-  }
+  window_tiling(c, n_q, &w);
+  const int32_t launch_rows = w.few ? n_q : (w.whole_heads ? ws::kMaxTiles : ws::kMaxClasses) * w.tile_rows;
   const int32_t t0 = w.win.t0;
   auto launch_at = [&](int32_t r0) {
     w.win.t0 = t0 + r0;

@@ -196,8 +196,7 @@ class Stream8:
         return q, pos, ref.norm_rope(q, pos, self.gamma)
 
 
-@pytest.mark.parametrize("fmt", FORMATS)
-@pytest.mark.parametrize("H,cond,units,video,audio,rows,few", [
+SHAPES = [
     (1, 0, 1, 1, 0, 1, False),       # one key, one row
     (2, 5, 1, 40, 3, 40, False),
     (3, 64, 3, 128, 4, 129, False),  # full pages
@@ -207,9 +206,16 @@ class Stream8:
     (3, 20, 3, 100, 4, 4, True),
     (2, 100, 9, 70, 5, 17, True),    # several key ranges
     (12, 64, 6, 252, 4, 1, True),
-])
-def test_attention_over_8_bits(ws, fmt, H, cond, units, video, audio, rows, few):
+]
+# splits: the call's own choice of kernel, or the video kernel's form over 1 or 3 key ranges
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("H,cond,units,video,audio,rows,few,splits",
+                         [(*c, n) for c in SHAPES for n in ((0,) if c[-1] else (0, 1, 3))])
+def test_attention_over_8_bits(ws, fmt, H, cond, units, video, audio, rows, few, splits):
     st = Stream8(ws, fmt, H, cond, units, video, audio, seed=rows)
+    st.cache.set_option(ws.WS_OPT_VIDEO_KV_SPLITS, splits)
     kinds = (ws.WS_KIND_COND, ws.WS_KIND_VIDEO) + ((ws.WS_KIND_AUDIO,) if few else ())
     q, pos, q64 = st.queries(rows, units - 1)
     call = st.cache.audio_attention if few else st.cache.unit_attention
@@ -239,9 +245,11 @@ def test_attention_over_8_bits(ws, fmt, H, cond, units, video, audio, rows, few)
 @pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("few", [False, True])
 @pytest.mark.parametrize("running_max", [0, 1])
-def test_wide_logits(ws, fmt, few, running_max):
+@pytest.mark.parametrize("splits", [0, 1, 2])
+def test_wide_logits(ws, fmt, few, running_max, splits):
     """Logits beyond the fixed shift's reach, and the running maximum forced."""
     st = Stream8(ws, fmt, 2, 10, 3, 150, 4, std=6.0 if not running_max else 1.0, seed=5)
+    st.cache.set_option(ws.WS_OPT_VIDEO_KV_SPLITS, splits)
     st.cache.set_option(ws.WS_OPT_VIDEO_RUNNING_MAX, running_max)
     kinds = (ws.WS_KIND_COND, ws.WS_KIND_VIDEO)
     rows = 20 if few else 150
@@ -250,6 +258,34 @@ def test_wide_logits(ws, fmt, few, running_max):
     (st.cache.audio_attention if few else st.cache.unit_attention)(
         q.cuda(), out, ws.mask_spec(2, kinds=kinds), positions=pos.cuda(), gamma=st.gamma.cuda())
     ref.check(out, *ref.attend(q64, *st.keys(2, kinds)))
+    st.cache.close()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("heads,rows", [(12, 920), (40, 252), (5, 1024)])
+def test_long_streams(ws, fmt, heads, rows):
+    """More pages than a workgroup's window of list entries, several tiles, heads cut
+    by the shares; every head against 64 bits on some rows, the same bits again, and
+    the bf16 kernel over what the cache stands for."""
+    st = Stream8(ws, fmt, heads, 100, 10, 920, 0, seed=rows)
+    kinds = (0, 1)
+    k, v = st.keys(9, kinds)
+    q = ref.normal(st.gen, rows, heads, D)
+    out = torch.full_like(q, float("nan")).cuda()
+    mask = ws.mask_spec(9, kinds=kinds)
+    st.cache.unit_attention(q.cuda(), out, mask, ws.WS_APPEND_RAW)
+    some = torch.randperm(rows, generator=st.gen)[:24]
+    ref.check(out[some.cuda()], *ref.attend(q[some].double(), k, v), label="some rows")
+    again = torch.empty_like(out)
+    st.cache.unit_attention(q.cuda(), again, mask, ws.WS_APPEND_RAW)
+    assert torch.equal(out, again)
+    plain = make(ws, heads, 10 * 15 + 4, "bf16")
+    for (u, kind), (kk, vv) in sorted(st.segs.items()):
+        plain.append(u, kind, kk.to(torch.bfloat16).cuda(), vv.to(torch.bfloat16).cuda())
+    plain.unit_attention(q.cuda(), again, mask, ws.WS_APPEND_RAW)
+    # two of the device's results, each within the bound; their 2-norm like two roundings
+    assert (out.float() - again.float()).norm() <= 2 * ref.U * again.float().norm()
+    plain.close()
     st.cache.close()
 
 

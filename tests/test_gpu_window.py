@@ -19,12 +19,15 @@ def run(ws, st, q, spec, **kw):
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
-@pytest.mark.parametrize("rows", [1, 4, 16, 17, 64, 65, 200])
+@pytest.mark.parametrize("rows,splits", [(1, 0), (4, 0), (16, 0), (17, 0), (64, 0), (65, 0), (200, 0),
+                                         (3, 1), (64, 2), (130, 3), (257, 1), (300, 2)])
 @pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (5, 64), (64, 0), (100, 3), (130, 65), (0, 0), (1000, 7)])
-def test_windows_and_sinks(ws, fmt, rows, window, sinks):
+def test_windows_and_sinks(ws, fmt, rows, splits, window, sinks):
     """Timeline: a 37-token slice, three units of 90 and 3 tokens (pages that end
-    inside a tile), rows at its end, from its start, across it and past it."""
+    inside a tile), rows at its end, from its start, across it and past it; the call's
+    own choice of kernel, or the video kernel's form over forced key ranges."""
     st = Stream8(ws, fmt, 2, 37, 3, 90, 3, seed=rows * 7 + window)
+    st.cache.set_option(ws.WS_OPT_VIDEO_KV_SPLITS, splits)
     kinds = (0, 1, 2)
     k, v = st.keys(2, kinds)
     n = k.shape[0]
@@ -70,10 +73,12 @@ def test_query_modes_and_unit_windows(ws, fmt, rows):
 @pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("rows", [5, 140])
 @pytest.mark.parametrize("running_max", [0, 1])
-def test_wide_logits(ws, fmt, rows, running_max):
+@pytest.mark.parametrize("splits", [0, 1, 2])
+def test_wide_logits(ws, fmt, rows, running_max, splits):
     """Rows under a running maximum, whose first visible keys come late: logits far
     from 0 on either side."""
     st = Stream8(ws, fmt, 2, 20, 3, 200, 0, std=1.0 if running_max else 6.0, seed=rows)
+    st.cache.set_option(ws.WS_OPT_VIDEO_KV_SPLITS, splits)
     st.cache.set_option(ws.WS_OPT_VIDEO_RUNNING_MAX, running_max)
     k, v = st.keys(2, (0, 1))
     n = k.shape[0]
@@ -90,12 +95,14 @@ def test_wide_logits(ws, fmt, rows, running_max):
 
 @pytest.mark.parametrize("rows", [6, 150])
 @pytest.mark.parametrize("bad", ["k", "v", "both"])
-def test_hidden_infinities_and_nans(ws, rows, bad):
+@pytest.mark.parametrize("splits", [0, 1, 2])
+def test_hidden_infinities_and_nans(ws, rows, bad, splits):
     """Values of any kind in tokens that a row does not see do not reach it, in pages
     that it sees part of (a bf16 cache; an 8-bit one stores none)."""
     gen = torch.Generator().manual_seed(rows)
     H, n = 2, 260
     cache = ws.Cache(H, 8, rope_max_pos=(8, 8, 8))
+    cache.set_option(ws.WS_OPT_VIDEO_KV_SPLITS, splits)
     k, v, q = (ref.normal(gen, n, H, D) for _ in range(3))
     q = q[:rows]
     first = 230 - rows - 20  # rows at 230 - rows .. 229, each over its last 20
@@ -121,6 +128,33 @@ def test_hidden_infinities_and_nans(ws, rows, bad):
     assert torch.isinf(got[sees, 0, 7]).all() and torch.isfinite(got[keep]).all()
     assert ((got - want).abs()[keep] <= bound[keep]).all()
     cache.close()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("heads,rows,window,sinks,causal", [
+    (12, 4096, 700, 64, True),   # a workgroup per tile and head
+    (40, 920, 3000, 256, False),
+    (3, 1500, 0, 0, True),       # classes, heads cut by the shares
+    (12, 1000, 4000, 300, True),
+    (1, 4096, 100, 0, True),
+])
+def test_many_tiles(ws, fmt, heads, rows, window, sinks, causal):
+    """Long runs of rows over long timelines, against 64 bits on some rows; the same
+    bits again, and independent of the other rows' number up to key ranges."""
+    st = Stream8(ws, fmt, heads, 256, 6, 920, 0, seed=heads, max_q=4096)
+    k, v = st.keys(5, (0, 1))
+    n = k.shape[0]
+    q = ref.normal(st.gen, rows, heads, D)
+    spec = ws.window_spec(5, window, sinks, causal=causal)
+    out = run(ws, st, q, spec)
+    some = torch.cat([torch.tensor([0, 1, rows - 1]), torch.randperm(rows, generator=st.gen)[:24]])
+    see = ref.window_mask(n, n - rows, rows, window, sinks, causal)[some]
+    ref.check(out[some.cuda()], *ref.attend(q[some].double(), k, v, see))
+    assert torch.equal(run(ws, st, q, spec), out)
+    part = run(ws, st, q[100:700], ws.window_spec(5, window, sinks, causal=causal, q_start=n - rows + 100))
+    # two results of the device, each within a few roundings of the exact one
+    assert (part.float() - out[100:700].float()).norm() <= 2 * ref.U * part.float().norm()
+    st.cache.close()
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
