@@ -267,11 +267,12 @@ WS_API ws_status ws_step_append(ws_cache* cache, int32_t n_kv, const ws_append_i
                                 int32_t n_q, const ws_query_item* qs, void* hip_stream);
 
 /* One segment of a ws_kv_gather call: k_out and v_out are device bf16
- * [n_tokens][H][128] with strides (tok_stride, head_stride), n_tokens the
- * segment's; one of them may be NULL. */
+ * [n_tokens][H][128] with strides (tok_stride, head_stride); one of them may be
+ * NULL.  n_tokens must be the segment's (WS_ERR_SHAPE). */
 typedef struct ws_gather_item {
   int32_t unit;
   ws_kind kind;
+  int32_t n_tokens;
   void* k_out;
   void* v_out;
   int64_t tok_stride;

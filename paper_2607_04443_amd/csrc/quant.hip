@@ -26,6 +26,8 @@ constexpr uint32_t kInfBits = 0x7f800000u;
 template <int kFmt>
 constexpr uint32_t kTooLarge = kFmt == kFmtInt8 ? 0x7a800000u : kInfBits;
 
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+
 // largest of the wave's values, in every lane
 template <int kRor>
 __device__ __forceinline__ uint32_t ror_umax(uint32_t v) {
@@ -39,8 +41,7 @@ __device__ __forceinline__ uint32_t wave_umax(uint32_t v) {
   return max(s[0], s[1]);
 }
 
-// The scale of a tile whose largest magnitude has the bits a, and its inverse
-// (exact for e4m3; for int8 rounded, quantise() corrects what that moves).
+// The scale of a tile whose largest magnitude has the bits a, and its inverse.
 template <int kFmt>
 __device__ __forceinline__ void tile_scale(uint32_t a, float& s, float& inv) {
   if constexpr (kFmt == kFmtInt8) {
@@ -55,23 +56,24 @@ __device__ __forceinline__ void tile_scale(uint32_t a, float& s, float& inv) {
   }
 }
 
-// Eight values to codes (two words), and the sum of the codes' squares.
+// Eight values to codes (two words), and |x|^2 of them (int8) or of what the codes
+// stand for (e4m3, in scales).
+//
+// int8: x inv + 1.5 2^23 + 128, rounded once, has code + 128 in its low byte.  Only
+// inv is off (2^-25), by at most 127 2^-25 < 2^-18 in the quotient; a bf16 value's
+// quotient by a scale of 16 bits is at least 2^-17 from the middle of two integers
+// where it is not in it (then s is a power of two and inv exact), so the code is the
+// nearest one.
 template <int kFmt>
-__device__ __forceinline__ u32x2 quantise8(const float (&x)[8], float s, float inv, float& norm2) {
+__device__ __forceinline__ u32x2 quantise8(const float (&x)[8], float inv, float& norm2) {
   u32x2 w;
   norm2 = 0.f;
   if constexpr (kFmt == kFmtInt8) {
-    // x inv is x / s within an ulp: the nearest integer, moved by one where the
-    // exact remainder says so
-    const float half = 0.5f * s;
     uint32_t c[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      float q = rintf(x[i] * inv);
-      const float e = fmaf(-q, s, x[i]);
-      q += e > half ? 1.f : e < -half ? -1.f : 0.f;
-      norm2 = fmaf(q, q, norm2);
-      c[i] = static_cast<uint32_t>(static_cast<int>(q) + 128);
+      norm2 = fmaf(x[i], x[i], norm2);
+      c[i] = __float_as_uint(fmaf(x[i], inv, 12583040.0f));
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -186,16 +188,17 @@ __device__ __forceinline__ void append_tile_q(const const_append_args A, int ite
   // largest magnitudes of the tile (as bits: infinities and NaN come out on top)
   uint32_t top[2];
   auto reduce = [&](int round) {
-    uint32_t mk = 0, mv = 0;
+    uint32_t mk = 0;
+    u16x2 pairs = {0, 0};
 #pragma unroll
     for (int pass = 0; pass < 4; ++pass)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         mk = max(mk, max(abs_bits(k[pass][2 * i]), abs_bits(k[pass][2 * i + 1])));
-        mv = max(mv, max(vx[pass][i] & 0x7fff0000u, (vx[pass][i] << 16) & 0x7fff0000u));
+        pairs = __builtin_elementwise_max(pairs, __builtin_bit_cast(u16x2, vx[pass][i] & 0x7fff7fffu));
       }
     mk = wave_umax(mk);
-    mv = wave_umax(mv);
+    const uint32_t mv = wave_umax(static_cast<uint32_t>(max(pairs[0], pairs[1])) << 16);
     if ((t & 63) == 0) {
       lds.top[round][0][wave] = mk;
       lds.top[round][1][wave] = mv;
@@ -237,9 +240,9 @@ __device__ __forceinline__ void append_tile_q(const const_append_args A, int ite
       v[2 * i + 1] = bf16_hi(vx[pass][i]);
     }
     float unused;
-    const u32x2 vw = quantise8<kFmt>(v, vs, vinv, unused);
+    const u32x2 vw = quantise8<kFmt>(v, vinv, unused);
     *reinterpret_cast<u32x2*>(&lds.v[row][(2 * c) ^ (4 * (row >> 3))]) = vw;
-    const u32x2 kw = quantise8<kFmt>(k[pass], ks, kinv, n2);
+    const u32x2 kw = quantise8<kFmt>(k[pass], kinv, n2);
     *reinterpret_cast<u32x2*>(kdst + k8_tile_index(row, 8 * c)) = kw;
     norm2 = fmaxf(norm2, row_sum(n2));
   }
@@ -262,10 +265,12 @@ __device__ __forceinline__ void append_tile_q(const const_append_args A, int ite
   if (t == 0) {
     A->kscale[tile] = ks;
     A->vscale[tile] = vs;
-    // the norm of the operands the attention makes of them: a code times the scale
-    // is rounded to bf16 for int8 (up by at most 2^-8), exact for e4m3
-    const float slack = kFmt == kFmtInt8 ? 1.008f : 1.0f;
-    A->knorm2[tile] = fmaxf(fmaxf(lds.norm2[0], lds.norm2[1]), fmaxf(lds.norm2[2], lds.norm2[3])) * slack * ks * ks;
+    // a bound on the norm of the operands the attention makes of them.  int8: each of
+    // 128 codes is off by half a scale at most, and code times scale rounded to bf16
+    // (up by at most 2^-8); e4m3: exact
+    const float top2 = fmaxf(fmaxf(lds.norm2[0], lds.norm2[1]), fmaxf(lds.norm2[2], lds.norm2[3]));
+    const float norm = kFmt == kFmtInt8 ? 1.004f * (sqrtf(top2) + 5.66f * ks) : sqrtf(top2) * ks;
+    A->knorm2[tile] = norm * norm;
   }
 }
 

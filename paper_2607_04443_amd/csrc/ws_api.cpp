@@ -1488,6 +1488,9 @@ ws_status ws_kv_gather(ws_cache* c, int32_t n, const ws_gather_item* items, void
     const ws::Segment* seg = c->pt.find(it.unit, it.kind);
     if (!seg)
       return fail(WS_ERR_UNKNOWN_UNIT, "item %d: no segment for unit %d kind %d", i, it.unit, static_cast<int>(it.kind));
+    if (it.n_tokens != seg->n_tokens)
+      return fail(WS_ERR_SHAPE, "item %d: %d tokens asked of unit %d kind %d (segment has %d)", i, it.n_tokens, it.unit,
+                  static_cast<int>(it.kind), seg->n_tokens);
     if (!it.k_out && !it.v_out) return fail(WS_ERR_INVALID_ARG, "item %d: no output", i);
     for (void* p : {it.k_out, it.v_out})
       if (p)

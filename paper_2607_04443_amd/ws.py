@@ -98,8 +98,8 @@ class ws_window_spec(ctypes.Structure):
 
 
 class ws_gather_item(ctypes.Structure):
-    _fields_ = [("unit", ctypes.c_int32), ("kind", ctypes.c_int32), ("k_out", ctypes.c_void_p),
-                ("v_out", ctypes.c_void_p), ("tok_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+    _fields_ = [("unit", ctypes.c_int32), ("kind", ctypes.c_int32), ("n_tokens", ctypes.c_int32),
+                ("k_out", ctypes.c_void_p), ("v_out", ctypes.c_void_p), ("tok_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
 
 
 class ws_attn_call(ctypes.Structure):
@@ -403,7 +403,7 @@ def ws_last_error() -> str:
 _APPEND_ITEM = struct.Struct("@PPqq" "iiiiPPf4x")
 _QUERY_DESC = struct.Struct("@i4xPPff")
 _QUERY_ITEM = struct.Struct("@Pqqi4x" "i4xPPff" "Pqq")
-_GATHER_ITEM = struct.Struct("@iiPPqq")
+_GATHER_ITEM = struct.Struct("@iii4xPPqq")
 _ATTN_CALL = struct.Struct("@Pqqi4x" "i4xPPff" "12s4x" "Pqq")
 for _layout, _type in ((_APPEND_ITEM, ws_append_item), (_QUERY_DESC, ws_query_desc),
                        (_QUERY_ITEM, ws_query_item), (_GATHER_ITEM, ws_gather_item), (_ATTN_CALL, ws_attn_call)):
@@ -530,17 +530,18 @@ class Cache:
     def gather(self, items, stream=None):
         """Segments out of the cache: dicts with unit, kind and k_out and/or v_out,
         bf16 [tokens, heads, 128] device tensors (of the same strides)."""
-        packed = []
+        packed, heads = [], self.num_heads
         for x in items:
-            unit, kind, k, v = x["unit"], x["kind"], x.get("k_out"), x.get("v_out")
-            outs = [(n, t) for n, t in (("k_out", k), ("v_out", v)) if t is not None]
-            n_tok = ws_segment_tokens(self.handle, unit, kind)
-            for name, t in outs:
-                if _rows(name, t) != outs[0][1].stride() or tuple(t.shape) != (n_tok, self.num_heads, 128):
-                    raise ValueError(f"{name} must be [{n_tok}, {self.num_heads}, 128], both of the same strides")
-            st = outs[0][1].stride() if outs else (0, 0)
-            packed.append(_GATHER_ITEM.pack(unit, kind, _ptr(k), _ptr(v), st[0], st[1]))
-        arr = (ws_gather_item * max(len(packed), 1)).from_buffer_copy(b"".join(packed) or bytes(_GATHER_ITEM.size))
+            k, v = x.get("k_out"), x.get("v_out")
+            st, shape = (0, 0), (0,)
+            for name, t in (("v_out", v), ("k_out", k)):
+                if t is not None:
+                    mine = _rows(name, t)
+                    if (len(shape) == 3 and (mine != st or t.shape != shape)) or t.shape[1] != heads:
+                        raise ValueError(f"{name} must have {heads} heads, k_out and v_out one shape and strides")
+                    st, shape = mine, t.shape
+            packed.append(_GATHER_ITEM.pack(x["unit"], x["kind"], shape[0], _ptr(k), _ptr(v), st[0], st[1]))
+        arr = (ws_gather_item * len(packed)).from_buffer_copy(b"".join(packed)) if packed else (ws_gather_item * 1)()
         _check(_lib.ws_kv_gather(self.handle, len(packed), arr, _stream_handle(stream)), "ws_kv_gather")
 
     def _attn(self, fn, q, out, mask, mode, positions, gamma, eps, scale, stream):

@@ -43,7 +43,7 @@ def test_struct_layouts(tmp_path):
     from paper_2607_04443_amd import ws
     src, exe = tmp_path / "p.c", tmp_path / "p"
     fields = {"ws_window_spec": ["mask", "window", "n_sink", "causal", "q_start"],
-              "ws_gather_item": ["unit", "kind", "k_out", "v_out", "tok_stride", "head_stride"]}
+              "ws_gather_item": ["unit", "kind", "n_tokens", "k_out", "v_out", "tok_stride", "head_stride"]}
     body = "".join(f'printf("%zu ", sizeof({t}));' + "".join(f'printf("%zu ", offsetof({t}, {f}));' for f in fs)
                    for t, fs in fields.items())
     src.write_text("#include <stddef.h>\n#include <stdio.h>\n#include \"ws.h\"\nint main(void) {" + body +

@@ -442,14 +442,17 @@ def test_refusals(ws):
         return status(ws.ws_kv_gather, cache.handle, [ws.ws_gather_item(*i) for i in items], 0)
 
     assert gather() == ws.WS_ERR_INVALID_ARG
-    assert gather(*[(0, 1, p, None, 256, 128)] * 17) == ws.WS_ERR_INVALID_ARG
-    assert gather((0, 3, p, None, 256, 128)) == ws.WS_ERR_INVALID_ARG
-    assert gather((0, 1, p, None, 256, 128), (0, 2, p, None, 256, 128)) == ws.WS_ERR_UNKNOWN_UNIT
-    assert gather((0, 1, None, None, 256, 128)) == ws.WS_ERR_INVALID_ARG
-    assert gather((0, 1, p + 2, None, 256, 128)) == ws.WS_ERR_INVALID_ARG
-    assert gather((0, 1, p, p, 252, 128)) == ws.WS_ERR_INVALID_ARG
-    assert gather((0, 1, p, None, 64, 128)) == ws.WS_ERR_INVALID_ARG
-    with pytest.raises(ValueError):
+    assert gather(*[(0, 1, 70, p, None, 256, 128)] * 17) == ws.WS_ERR_INVALID_ARG
+    assert gather((0, 3, 70, p, None, 256, 128)) == ws.WS_ERR_INVALID_ARG
+    assert gather((0, 1, 70, p, None, 256, 128), (0, 2, 70, p, None, 256, 128)) == ws.WS_ERR_UNKNOWN_UNIT
+    assert gather((0, 1, 69, p, None, 256, 128)) == ws.WS_ERR_SHAPE
+    assert gather((0, 1, 70, None, None, 256, 128)) == ws.WS_ERR_INVALID_ARG
+    assert gather((0, 1, 70, p + 2, None, 256, 128)) == ws.WS_ERR_INVALID_ARG
+    assert gather((0, 1, 70, p, p, 252, 128)) == ws.WS_ERR_INVALID_ARG
+    assert gather((0, 1, 70, p, None, 64, 128)) == ws.WS_ERR_INVALID_ARG
+    with pytest.raises(ws.WsError):
+        cache.gather([])
+    with pytest.raises(ws.WsError):
         cache.gather([dict(unit=0, kind=1, k_out=out[:69])])
     with pytest.raises(ValueError):
         cache.gather([dict(unit=0, kind=1, k_out=out, v_out=torch.empty(70, 4, D, dtype=torch.bfloat16,
