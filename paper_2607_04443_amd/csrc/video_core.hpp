@@ -198,7 +198,7 @@ struct Stream8 {
   uint32_t ks[2], vs[2]; // scales (bits) of the window's units
   const float* kscale;
   const float* vscale;
-  uint32_t load;         // this lane's source byte offset within 4 KB of a tile
+  uint32_t load[2];      // this lane's source byte offsets within a tile's halves
   uint32_t wk, wv;       // and its write offsets within a stage (first chunk)
 };
 struct StreamWin {
@@ -375,11 +375,12 @@ __device__ __forceinline__ void set_load(const VideoStream<P>& s, uint32_t e, ui
 // two 16-byte chunks of an LDS tile each.  One word of bf16 at a time: word n of 32
 // is word n % 8 of part n / 8; a full chunk is written, a part whose codes are all
 // used is loaded again (of the page three ahead).
+typedef const __attribute__((address_space(1))) char* global_bytes;
 template <int kPart, class P>
 __device__ __forceinline__ void load_part(VideoStream<P>& s, const PageCtx<P>& c) {
   // (global: a flat load would count among the LDS accesses too)
-  const uint64_t base = reinterpret_cast<uint64_t>(kPart < 2 ? c.ldk : c.ldv) + 4096 * (kPart & 1);
-  s.raw[kPart] = *(const __attribute__((address_space(1))) u32x4*)(base + s.load);
+  const global_bytes base = (global_bytes)(kPart < 2 ? c.ldk : c.ldv);
+  s.raw[kPart] = *(const __attribute__((address_space(1))) u32x4*)(base + s.load[kPart & 1]);
 }
 template <int kWord, bool kAgain, class P>
 __device__ __forceinline__ void stage_word(VideoStream<P>& s, const PageCtx<P>& c, u32x4& chunk) {
@@ -1727,7 +1728,8 @@ __device__ __forceinline__ void unit_attn(const AttnArgs& a) {
       const uint32_t t = 64u * wave + lane, key = t >> 2, part = t & 3;
       // K: row 16 tile + m of the key, chunks 2 part (and 8 further, and the odd ones)
       const uint32_t tile = 2 * (key >> 5) + ((key >> 2) & 1), row = 4 * ((key >> 3) & 3) + (key & 3);
-      s.load = 16u * t;
+      s.load[0] = 16u * t;
+      s.load[1] = opaque(16u * t + 4096u);  // (a register of its own: an offset beside a scalar base)
       s.wk = lds + 256u * (16u * tile + row) + 16u * ((2u * part) ^ row);
       s.wv = lds + kStageV + 128u * key + 16u * ((2u * part) ^ ((key >> 1) & 7));  // (V^T: dim t / 4)
     }
