@@ -51,6 +51,7 @@ struct Path {
   static constexpr bool k8 = kFormat != kFmtBf16;
   static constexpr bool kWin = kWindow;
   static constexpr bool kPlain = kFormat == kFmtBf16 && !kWindow;
+  static constexpr bool kQ8 = kFormat == kFmtE4m3;  // S by 8-bit products (VideoState)
 };
 using PlainPath = Path<kFmtBf16, false>;
 template <int>
@@ -91,6 +92,7 @@ constexpr uint32_t kStageBytes = 2 * kPageHeadElems * 2;
 constexpr uint32_t kStageV = kPageHeadElems * 2;  // offset of the V tile
 __shared__ __attribute__((aligned(1024))) uint16_t g_stages[kStages * 2 * kPageHeadElems];
 
+typedef int i32x8 __attribute__((ext_vector_type(8)));
 __device__ __forceinline__ bf16x8 as_bf16x8(u32x4 v) { return __builtin_bit_cast(bf16x8, v); }
 
 // The call's visible page list: in device memory, or in the kernel
@@ -145,6 +147,12 @@ __device__ __forceinline__ void scale_acc(f32x4& d, float f) {
     d[r] = x;
   }
 }
+// S of a K tile's codes (a: 32 dims of a key per lane) and one term of the queries, on
+// the scales 2^(k_exp - 127) and byte kTerm of q_exp.
+template <int kTerm>
+__device__ __forceinline__ void mfma_s8(f32x4& d, const i32x8& a, const i32x8& b, const f32x4& c, int k_exp, int q_exp) {
+  d = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, k_exp, kTerm, q_exp);
+}
 // A value the compiler cannot carry over from an earlier computation: the
 // epilogue recomputes its addresses instead of keeping them live across the
 // page loop.
@@ -171,13 +179,10 @@ struct Ctx8 {
   uint32_t ks, vs;         // scales (bits) of the page two ahead (its codes are in the registers)
   uint32_t ks_load, vs_load;  // of the page three ahead
   uint32_t wk, wv;         // LDS offsets of this lane's writes of the page two ahead
-};
-struct CtxWin {
-  int start;               // the page's first timeline index
-  int edge;                // what hides slots of it from rows of the wave (kEdge*)
+  uint32_t vs1, k_exp;     // (e4m3) word of the page one ahead; exponent byte of the current page's K scale
 };
 template <class P>
-struct PageCtx : std::conditional_t<P::k8, Ctx8, Nothing<0>>, std::conditional_t<P::kWin, CtxWin, Nothing<1>> {
+struct PageCtx : std::conditional_t<P::k8, Ctx8, Nothing<0>> {
   uint32_t k[4];        // LDS offsets of this lane's operand reads: K, per k-step (key tile t: + 4096 t)
   uint32_t v;           // V^T chunk 0 (d tile dt: + 2048 dt)
   uint32_t vp;          // V^T chunk 1 of the page before
@@ -195,7 +200,7 @@ struct PageCtx : std::conditional_t<P::k8, Ctx8, Nothing<0>>, std::conditional_t
 // counter that only a full wait can order).
 struct Stream8 {
   u32x4 raw[4];          // codes of the page two ahead: K dims 0-63 and 64-127, V dims 0-63 and 64-127
-  uint32_t ks[2], vs[2]; // scales (bits) of the window's units
+  uint32_t ks[2], vs[2]; // scales (bits) of the window's units (e4m3: both in vs, scale_word)
   const float* kscale;
   const float* vscale;
   uint32_t load[2];      // this lane's source byte offsets within a tile's halves
@@ -249,13 +254,39 @@ __device__ __forceinline__ uint32_t valid_of(int y) {
   return P::kWin ? static_cast<uint32_t>(y) & 127u : static_cast<uint32_t>(y);
 }
 __device__ __forceinline__ int start_of(int y) { return static_cast<int>(static_cast<uint32_t>(y) >> 7); }
+// What hides slots of a page that starts at timeline index `start` from rows of the
+// wave, kEdge* bits: a row's end (the page's own, or a row's last key), and a row's
+// first key, in a page with sinks or without.  (Each a pass of its own over the S
+// tiles, two or three instructions a value: all three conditions at once take five.)
+constexpr int kEdgeHi = 1, kEdgeLo = 2, kEdgeSinks = 4;
+template <class P>
+__device__ __forceinline__ int page_edge(const VideoStream<P>& s, int start, int valid) {
+  const int end = start + kPageTokens;
+  const bool lo_hidden = (start < s.lo_all) & (end > s.win.sinks), hi_hidden = (valid < kPageTokens) | (end > s.hi_all);
+  const int lo = lo_hidden ? (start < s.win.sinks ? kEdgeSinks : kEdgeLo) : 0, hi = hi_hidden ? kEdgeHi : 0;
+  return lo | hi;
+}
+// The low 7 bits of a unit's entry: the page's valid tokens, and, with a window, 65
+// for a full page with an edge (a shorter one has one): an edge is looked for once per
+// unit, by the lane that holds it, and the page loop compares with 64.
+template <class P>
+__device__ __forceinline__ uint32_t entry_valid(const VideoStream<P>& s, int y) {
+  uint32_t v = valid_of<P>(y);
+  if constexpr (P::kWin) v = v == kPageTokens && page_edge(s, start_of(y), kPageTokens) != 0 ? kPageTokens + 1 : v;
+  return v;
+}
+// e4m3: both scales of a page are powers of two; V's bits with K's exponent byte.
+template <class P>
+__device__ __forceinline__ uint32_t scale_word(const VideoStream<P>& s, uint32_t tile) {
+  return __float_as_uint(s.vscale[tile]) | (__float_as_uint(s.kscale[tile]) >> 23);
+}
 template <class P>
 __device__ __forceinline__ uint32_t stream_entry(const VideoStream<P>& s, int k, int* start = nullptr) {
   const uint32_t x = s.lo + min(k, s.n - 1), head = fast_div(x, s.div_pages);
   const int pi = stream_place(s, static_cast<int>(x - head * s.n_pages));
   const int y = s.pages[pi].y;
   if (start) *start = start_of(y);
-  return ((s.pages[pi].x * s.num_heads + head_of(s, head)) << 7) | valid_of<P>(y);
+  return ((s.pages[pi].x * s.num_heads + head_of(s, head)) << 7) | entry_valid(s, y);
 }
 // The first window: its list entries requested, then combined.
 template <class P>
@@ -273,7 +304,7 @@ template <class P>
 __device__ __forceinline__ void stream_combine(VideoStream<P>& s) {
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
-    s.ent[k] = ((s.raw_page[k] * s.num_heads + s.raw_head[k]) << 7) | valid_of<P>(s.raw_valid[k]);
+    s.ent[k] = ((s.raw_page[k] * s.num_heads + s.raw_head[k]) << 7) | entry_valid(s, s.raw_valid[k]);
     if constexpr (P::kWin) s.start[k] = start_of(s.raw_valid[k]);
   }
 }
@@ -302,7 +333,11 @@ __device__ __forceinline__ void stream_reach(VideoStream<P>& s) {
       asm volatile("" : "+v"(start));
       if (k & 64) s.start[1] = start; else s.start[0] = start;
     }
-    if constexpr (P::k8) {
+    if constexpr (P::kQ8) {
+      uint32_t vs = scale_word(s, e >> 7);
+      asm volatile("" : "+v"(vs));
+      if (k & 64) s.vs[1] = vs; else s.vs[0] = vs;
+    } else if constexpr (P::k8) {
       uint32_t ks = __float_as_uint(s.kscale[e >> 7]), vs = __float_as_uint(s.vscale[e >> 7]);
       asm volatile("" : "+v"(ks), "+v"(vs));
       if (k & 64) s.ks[1] = ks; else s.ks[0] = ks;
@@ -382,10 +417,24 @@ __device__ __forceinline__ void load_part(VideoStream<P>& s, const PageCtx<P>& c
   const global_bytes base = (global_bytes)(kPart < 2 ? c.ldk : c.ldv);
   s.raw[kPart] = *(const __attribute__((address_space(1))) u32x4*)(base + s.load[kPart & 1]);
 }
+// (The swizzles of K: chunk c of row m at position c ^ swap_low_bits(m).  e4m3: a part
+// goes as it is, [64 rows][8 chunks], rows as above, chunk c (dims 16 c ..) at position
+// c ^ codes_swizzle(m).)
+__device__ __forceinline__ uint32_t swap_low_bits(uint32_t x) { return (x & ~3u) | ((x & 1) << 1) | ((x >> 1) & 1); }
+__device__ __forceinline__ uint32_t codes_swizzle(uint32_t m) {
+  return 4 * ((m >> 1) & 1) + 2 * (((m >> 2) ^ (m >> 3)) & 1) + ((m >> 2) & 1);
+}
+template <int kPart, bool kAgain, class P>
+__device__ __forceinline__ void stage_codes(VideoStream<P>& s, const PageCtx<P>& c) {
+  *(__attribute__((address_space(3))) u32x4*)(c.wk ^ (64u * kPart)) = s.raw[kPart];
+  if constexpr (kAgain) load_part<kPart>(s, c);
+}
 template <int kWord, bool kAgain, class P>
 __device__ __forceinline__ void stage_word(VideoStream<P>& s, const PageCtx<P>& c, u32x4& chunk) {
   constexpr int part = kWord >> 3, h = (kWord >> 2) & 1;
-  const QuantScale q = quant_scale<P::kFmt>(__uint_as_float(part < 2 ? c.ks : c.vs));
+  uint32_t scale = part < 2 ? c.ks : c.vs;
+  if constexpr (P::kQ8) scale &= 0xff800000u;
+  const QuantScale q = quant_scale<P::kFmt>(__uint_as_float(scale));
   uint32_t w = codes_to_bf16<P::kFmt, kWord & 1>(s.raw[part][(kWord & 7) >> 1], q);
   asm volatile("" : "+v"(w));
   chunk[kWord & 3] = w;
@@ -398,7 +447,13 @@ __device__ __forceinline__ void stage_word(VideoStream<P>& s, const PageCtx<P>& 
 template <bool kAgain, class P>
 __device__ __forceinline__ void stage_page(VideoStream<P>& s, const PageCtx<P>& c) {
   u32x4 chunk;
-  static_for<32>([&](auto n) __attribute__((always_inline)) { stage_word<decltype(n)::value, kAgain>(s, c, chunk); });
+  if constexpr (P::kQ8) {
+    stage_codes<0, kAgain>(s, c);
+    stage_codes<1, kAgain>(s, c);
+  }
+  static_for<P::kQ8 ? 16 : 32>([&](auto n) __attribute__((always_inline)) {
+    stage_word<decltype(n)::value + (P::kQ8 ? 16 : 0), kAgain>(s, c, chunk);
+  });
 }
 // Waits for the wave's LDS accesses, all or all but the last three.
 __device__ __forceinline__ void wait_lds() { __builtin_amdgcn_s_waitcnt(0xC07F); }
@@ -434,19 +489,6 @@ __device__ __forceinline__ void set_reads(const VideoStream<P>& s, uint32_t stag
   c.vp = (s.v_read + ring_add(stage, kStages - 1)) ^ 64u;
 }
 
-// What hides slots of a page from some row of the wave: its end (the page's valid
-// tokens, or a row's last key), and a row's first key, in a page with sinks or
-// without.  (Each a pass of its own over the S tiles, two or three instructions a
-// value: all three conditions at once take five.)
-constexpr int kEdgeHi = 1, kEdgeLo = 2, kEdgeSinks = 4;
-template <class P>
-__device__ __forceinline__ int page_edge(const VideoStream<P>& s, int start, int valid) {
-  const int end = start + kPageTokens;
-  const int lo = (start < s.lo_all) & (end > s.win.sinks) ? (start < s.win.sinks ? kEdgeSinks : kEdgeLo) : 0;
-  const int hi = (valid < kPageTokens) | (end > s.hi_all) ? kEdgeHi : 0;
-  return __builtin_amdgcn_readfirstlane(lo | hi);
-}
-
 // Starts the stream: key norms of its first window, the loads of its first
 // three pages, and the context of its first page.  (Past a stream's end the
 // last page is loaded once more, into a stage nothing reads.)
@@ -458,8 +500,12 @@ __device__ __forceinline__ void stream_start(const AttnArgs& a, VideoStream<P>& 
   if constexpr (P::k8) {
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-      s.ks[k] = __float_as_uint(a.kscale[s.ent[k] >> 7]);
-      s.vs[k] = __float_as_uint(a.vscale[s.ent[k] >> 7]);
+      if constexpr (P::kQ8) {
+        s.vs[k] = scale_word(s, s.ent[k] >> 7);
+      } else {
+        s.ks[k] = __float_as_uint(s.kscale[s.ent[k] >> 7]);
+        s.vs[k] = __float_as_uint(s.vscale[s.ent[k] >> 7]);
+      }
     }
   }
   if (s.n == 0) return;
@@ -470,11 +516,16 @@ __device__ __forceinline__ void stream_start(const AttnArgs& a, VideoStream<P>& 
     s.valid |= (e & 127u) << (8 * k);
     set_load(s, e, k * kStageBytes, s.c);
     if constexpr (P::k8) {  // pages 0 and 1 to their stages, page 2 to the registers
-      s.c.ks_load = peek_lanes(s.ks, min(k, s.n - 1));
+      if constexpr (!P::kQ8) s.c.ks_load = peek_lanes(s.ks, min(k, s.n - 1));
       s.c.vs_load = peek_lanes(s.vs, min(k, s.n - 1));
       if (k < 3) {
         static_for<4>([&](auto i) __attribute__((always_inline)) { load_part<decltype(i)::value>(s, s.c); });
-        s.c.ks = s.c.ks_load;
+        if constexpr (P::kQ8) {
+          s.c.k_exp = s.c.vs1;
+          s.c.vs1 = s.c.vs;
+        } else {
+          s.c.ks = s.c.ks_load;
+        }
         s.c.vs = s.c.vs_load;
         s.c.wk = s.wk + k * kStageBytes;
         s.c.wv = s.wv + k * kStageBytes;
@@ -484,16 +535,31 @@ __device__ __forceinline__ void stream_start(const AttnArgs& a, VideoStream<P>& 
       if (k < 3) issue_page(s, s.c);
     }
   }
-  if constexpr (P::kWin) {
-    s.c.start = peek_lanes(s.start, 0);
-    s.c.edge = page_edge(s, s.c.start, static_cast<int>(s.valid & 127u));
-  }
   set_reads(s, 0, s.c);
 }
 
-// A wave's query rows: kQT subtiles of 16.
+// e4m3 pages: S = K Q''^T is taken from the codes as they are, by
+// v_mfma_scale_f32_16x16x128_f8f6f4 at twice the bf16 rate.  Q'' is split into two
+// e4m3 terms of a row scale 2^f, q1 = e4m3(Q'' / 2^f) and q2 = e4m3((Q'' / 2^f - q1)
+// 16): Q'' = (q1 + q2 / 16) 2^f to within 2^-8 of itself, as one more rounding to
+// bf16 would be.  The products' scale operands carry the page's K scale and the row's
+// 2^f and 2^(f - 4), so S comes out as before.  (The 128 products of an instruction
+// are added with about 17 bits below the largest: measured against 64 bits, 3e-5 of
+// the sum of magnitudes at most on random codes of the whole range, exact on codes
+// within 2^3 of each other.)  A page of 64 rows then takes 104 MFMAs of the same total
+// length instead of 136, 24 operand reads instead of 32, and no conversion of K: 361
+// instructions a page where one wave fills a SIMD (bf16 pages: 378), where converting K
+// to bf16 as well took 445.
 template <int kQT>
-struct VideoState {
+struct StateQ8 {
+  i32x8 pair[2];     // operands in flight: K tiles ...
+  u32x4 single[2];   // ... and, with the pairs' halves, V^T: slot = read % 6
+  i32x8 q8[kQT][2];  // the row's two terms (accumulation registers)
+  int q_exp[kQT];    // and their exponent bytes
+};
+// A wave's query rows: kQT subtiles of 16.
+template <int kQT, class P>
+struct VideoState : std::conditional_t<P::kQ8, StateQ8<kQT>, Nothing<4>> {
   f32x4 o[8][kQT];    // O^T[16 dt + 4 g + r][q]  (accumulation registers)
   f32x4 l[kQT];       // row sums, the same in every register and lane group
   f32x4 s_init[kQT];  // -m in every register: the S tiles start at the exp2 argument
@@ -519,8 +585,15 @@ constexpr int kRingAhead = 3;
 
 // The queries live in accumulation registers (an MFMA reads its operands from
 // either bank), which leaves the vector registers to the softmax.
-template <int kQT>
-__device__ __forceinline__ void pin_queries(VideoState<kQT>& st) {
+template <int kQT, class P>
+__device__ __forceinline__ void pin_queries(VideoState<kQT, P>& st) {
+  if constexpr (P::kQ8) {
+#pragma unroll
+    for (int j = 0; j < kQT; ++j)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) asm volatile("" : "+a"(st.q8[j][t]));
+    return;
+  }
 #pragma unroll
   for (int j = 0; j < kQT; ++j)
 #pragma unroll
@@ -539,8 +612,8 @@ __device__ __forceinline__ void put_word(u32x4& p, int word, float lo, float hi)
 // O and l of the rows raised at the last check, scaled to their new m.  No MFMA
 // on them may be under way (the page loop: the last one was issued eight steps
 // before).
-template <int kQT>
-__device__ __forceinline__ void scale_raised(VideoState<kQT>& st) {
+template <int kQT, class P>
+__device__ __forceinline__ void scale_raised(VideoState<kQT, P>& st) {
   if (st.raised == 0) return;
   sched_fence();
 #pragma unroll
@@ -603,12 +676,10 @@ __device__ __forceinline__ void scale_raised(VideoState<kQT>& st) {
 // Windows: what hides keys is a page's edge flag, the wave's own.  A row may meet
 // its first visible key late: until then its m is unset and its S the bare logits.
 template <int kQT, bool kFirst, bool kLazy, class P>
-__device__ __forceinline__ void video_iter(VideoState<kQT>& st, VideoStream<P>& s) {
+__device__ __forceinline__ void video_iter(VideoState<kQT, P>& st, VideoStream<P>& s) {
   const int n_valid = static_cast<int>(s.valid & 0xffu);
   const PageCtx<P> c = s.c;
-  bool tail;
-  if constexpr (P::kWin) tail = c.edge != 0;
-  else tail = n_valid < kPageTokens;
+  const bool tail = P::kWin ? n_valid != kPageTokens : n_valid < kPageTokens;
   PageCtx<P> nx;
   [[maybe_unused]] u32x4 chunk;
   pin_queries(st);
@@ -623,8 +694,54 @@ __device__ __forceinline__ void video_iter(VideoState<kQT>& st, VideoStream<P>& 
     else if constexpr (n < 24) return lds_read16(c.k[n & 3] + 4096u * (2 + ((n - 16) >> 2)));
     else return lds_read16(c.v + 2048u * (n - 24));
   };
+  // e4m3: read n of a page's 24 (K tiles 0 and 1 two each, V^T chunk 1 of the page
+  // before eight, K tiles 2 and 3, V^T chunk 0; 24 and 25 are the next page's first),
+  // into slot n % 6; the read that step o issues is three or four steps ahead of its
+  // use and behind the last use of the slot's former one
+  [[maybe_unused]] auto q8_read = [&](auto nc) __attribute__((always_inline)) {
+    constexpr int n = decltype(nc)::value, slot = n % 6;
+    if constexpr (P::kQ8) {
+      uint32_t at;
+      if constexpr (n >= 24) at = nx.k[n - 24];
+      else if constexpr (n >= 16) at = c.v + 2048u * (n - 16);
+      else if constexpr (n >= 12) at = c.k[n & 1] + 2048u * (2 + ((n - 12) >> 1));
+      else if constexpr (n >= 4) at = c.vp + 2048u * (n - 4);
+      else at = c.k[n & 1] + 2048u * (n >> 1);
+      const u32x4 w = *(const __attribute__((address_space(3))) u32x4*)at;
+      if constexpr (slot < 4) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) st.pair[slot >> 1][4 * (slot & 1) + i] = static_cast<int>(w[i]);
+      } else {
+        st.single[slot - 4] = w;
+      }
+    }
+  };
+  [[maybe_unused]] auto q8_operand = [&](auto nc) __attribute__((always_inline)) {
+    constexpr int slot = decltype(nc)::value % 6;
+    u32x4 w = {0u, 0u, 0u, 0u};
+    if constexpr (P::kQ8) {
+      if constexpr (slot < 4) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = static_cast<uint32_t>(st.pair[slot >> 1][4 * (slot & 1) + i]);
+      } else {
+        w = st.single[slot - 4];
+      }
+    }
+    return as_bf16x8(w);
+  };
+  // operand of a P*V step
+  auto pv_operand = [&](auto oc) __attribute__((always_inline)) {
+    constexpr int o = decltype(oc)::value;
+    if constexpr (P::kQ8) return q8_operand(Const<(o < 16 ? o - 4 : o - 8)>{});
+    else return st.ring[o & 3];
+  };
   if constexpr (kFirst) {
-    static_for<kRingAhead>([&](auto n) __attribute__((always_inline)) { st.ring[decltype(n)::value] = oread(n); });
+    if constexpr (P::kQ8) {
+      q8_read(Const<0>{});
+      q8_read(Const<1>{});
+    } else {
+      static_for<kRingAhead>([&](auto n) __attribute__((always_inline)) { st.ring[decltype(n)::value] = oread(n); });
+    }
   }
   f32x4 sa[4][kQT];
   u32x4 p0[kQT], p1n[kQT];
@@ -724,10 +841,13 @@ __device__ __forceinline__ void video_iter(VideoState<kQT>& st, VideoStream<P>& 
       // 0 (a correction subtracted from the row sum afterwards would cancel
       // for rows whose logits all sit far below the shift)
       const int off = 8 * (opaque(s.lane) >> 4);
-      const int lim = n_valid - off;
+      [[maybe_unused]] int lim = n_valid - off;
       if constexpr (P::kWin) {
         // row by row: keys at or past hi, and from the sinks' end up to lo, are hidden
-        const int at = c.start + off;
+        const int start = peek_lanes(s.start, s.at), valid = min(n_valid, kPageTokens);
+        const int edge = __builtin_amdgcn_readfirstlane(page_edge(s, start, valid));
+        const int at = start + off;
+        lim = valid - off;
         auto hide = [&](auto&& hidden) __attribute__((always_inline)) {
 #pragma unroll
           for (int j = 0; j < kQT; ++j) {
@@ -739,11 +859,11 @@ __device__ __forceinline__ void video_iter(VideoState<kQT>& st, VideoStream<P>& 
                 sa[t][j][r] = hidden(rr, 32 * (t >> 1) + 4 * (t & 1) + r) ? kNegInf : sa[t][j][r];
           }
         };
-        if (c.edge & kEdgeHi)
+        if (edge & kEdgeHi)
           hide([&](const RowRange& rr, int slot) __attribute__((always_inline)) { return slot >= min(lim, rr.hi - at); });
-        if (c.edge & kEdgeLo)
+        if (edge & kEdgeLo)
           hide([&](const RowRange& rr, int slot) __attribute__((always_inline)) { return slot < rr.lo - at; });
-        if (c.edge & kEdgeSinks) {
+        if (edge & kEdgeSinks) {
           const int sk = s.win.sinks - at;
           hide([&](const RowRange& rr, int slot) __attribute__((always_inline)) { return slot >= sk && slot < rr.lo - at; });
         }
@@ -801,56 +921,81 @@ __device__ __forceinline__ void video_iter(VideoState<kQT>& st, VideoStream<P>& 
     }
     if constexpr (o == 15) { st_next = ring_add(s.stage, 1); pin_s(st_next); }
     constexpr uint32_t tile_shift = P::k8 ? kCodeTileShift : 14;
-    if constexpr (o == 16) {
+    constexpr int ld_step = P::k8 ? 28 : 16;
+    if constexpr (o == ld_step) {
       nx.ldk = reinterpret_cast<const uint16_t*>(reinterpret_cast<uint64_t>(s.kpool) + (static_cast<uint64_t>(ent >> 7) << tile_shift));
       pin_s(nx.ldk);
     }
-    if constexpr (o == 17) {
+    if constexpr (o == ld_step + 1) {
       nx.ldv = reinterpret_cast<const uint16_t*>(reinterpret_cast<uint64_t>(s.vpool) + (static_cast<uint64_t>(ent >> 7) << tile_shift));
       pin_s(nx.ldv);
     }
     if constexpr (P::k8) {
       if constexpr (o == 15) {
-        nx.ks = c.ks_load;
+        if constexpr (P::kQ8) {
+          nx.k_exp = c.vs1;
+          nx.vs1 = c.vs;
+        } else {
+          nx.ks = c.ks_load;
+        }
         nx.vs = c.vs_load;
       }
-      if constexpr (o == 16) { nx.ks_load = peek_lanes(s.ks, look); pin_s(nx.ks_load); }
-      if constexpr (o == 17) { nx.vs_load = peek_lanes(s.vs, look); pin_s(nx.vs_load); }
+      if constexpr (o == 24 && !P::kQ8) { nx.ks_load = __builtin_amdgcn_readlane(s.ks[0], look & 63); pin_s(nx.ks_load); }
+      if constexpr (o == 25 && !P::kQ8) {
+        const uint32_t w1 = __builtin_amdgcn_readlane(s.ks[1], look & 63);
+        nx.ks_load = (look & 64) ? w1 : nx.ks_load;
+        pin_s(nx.ks_load);
+      }
+      if constexpr (o == 26) { nx.vs_load = __builtin_amdgcn_readlane(s.vs[0], look & 63); pin_s(nx.vs_load); }
+      if constexpr (o == 27) {
+        const uint32_t w1 = __builtin_amdgcn_readlane(s.vs[1], look & 63);
+        nx.vs_load = (look & 64) ? w1 : nx.vs_load;
+        pin_s(nx.vs_load);
+      }
       if constexpr (o == 18) { nx.wk = s.wk + ring_add(st_next, 2); pin_v(nx.wk); }
       if constexpr (o == 19) { nx.wv = s.wv + ring_add(st_next, 2); pin_v(nx.wv); }
     } else {
       if constexpr (o == 18) { nx.lds = s.lds0 + ring_add(st_next, 3); pin_s(nx.lds); }
     }
-    if constexpr (P::kWin) {
-      if constexpr (o == 25) { nx.start = peek_lanes(s.start, min(s.at + 1, s.n - 1)); pin_s(nx.start); }
-      if constexpr (o == 26) { nx.edge = page_edge(s, nx.start, static_cast<int>((s.valid >> 8) & 0xffu)); }
-    }
     if constexpr (o == 19) { nx.k[0] = s.k_read + st_next; pin_v(nx.k[0]); }
     if constexpr (o == 20) { nx.k[1] = nx.k[0] ^ 64u; pin_v(nx.k[1]); }
-    if constexpr (o == 21) { nx.k[2] = nx.k[0] ^ 128u; pin_v(nx.k[2]); }
-    if constexpr (o == 22) { nx.k[3] = nx.k[0] ^ 192u; pin_v(nx.k[3]); }
+    if constexpr (o == 21 && !P::kQ8) { nx.k[2] = nx.k[0] ^ 128u; pin_v(nx.k[2]); }
+    if constexpr (o == 22 && !P::kQ8) { nx.k[3] = nx.k[0] ^ 192u; pin_v(nx.k[3]); }
     if constexpr (o == 23) { nx.v = s.v_read + st_next; pin_v(nx.v); }
     if constexpr (o == 24) { nx.vp = c.v ^ 64u; pin_v(nx.vp); }
     if constexpr (o == 28) { s.valid = __builtin_amdgcn_readfirstlane((s.valid >> 8) | ((ent & 127u) << 24)); }
   };
   static_for<32>([&](auto oc) __attribute__((always_inline)) {
     constexpr int o = decltype(oc)::value;
-    const bf16x8 a = st.ring[o & 3];
     static_for<kQT>([&](auto jc) __attribute__((always_inline)) {
       constexpr int j = decltype(jc)::value, k = j >> 1;
       constexpr bool even = (j & 1) == 0, last = j == kQT - 1;
       // ---- the MFMA ----
-      if constexpr (o < 8 || (o >= 16 && o < 24)) {
+      constexpr bool s_step = o < 8 || (o >= 16 && o < 24);
+      if constexpr (s_step) {
         constexpr int t = (o < 8 ? 0 : 2) + ((o & 7) >> 2);
-        if constexpr ((o & 3) == 0) mfma_s(sa[t][j], a, st.q[j][0], st.s_init[j]);
-        else mfma_s(sa[t][j], a, st.q[j][o & 3], sa[t][j]);
-        pin_v(sa[t][j]);
+        if constexpr (P::kQ8) {
+          // a tile's 2 kQT products, each as long as two of the slots
+          constexpr int slot = (o & 3) * kQT + j, jj = slot / 2 % kQT, term = slot / 2 / kQT;
+          if constexpr (slot % 2 == 0) {
+            mfma_s8<term>(sa[t][jj], st.pair[t & 1], st.q8[jj][term], term == 0 ? st.s_init[jj] : sa[t][jj],
+                          static_cast<int>(c.k_exp), st.q_exp[jj]);
+            pin_v(sa[t][jj]);
+          }
+        } else {
+          const bf16x8 a = st.ring[o & 3];
+          if constexpr ((o & 3) == 0) mfma_s(sa[t][j], a, st.q[j][0], st.s_init[j]);
+          else mfma_s(sa[t][j], a, st.q[j][o & 3], sa[t][j]);
+          pin_v(sa[t][j]);
+        }
       } else if constexpr (o < 16) {
+        const bf16x8 a = pv_operand(oc);
         if constexpr (!kFirst) {
           mfma_o(st.o[o - 8][j], a, as_bf16x8(st.p1[j]));
           if constexpr (o == 15) mfma_o(st.l[j], as_bf16x8(st.ones), as_bf16x8(st.p1[j]));
         }
       } else {
+        const bf16x8 a = pv_operand(oc);
         if constexpr (kFirst) mfma_o_first(st.o[o - 24][j], a, as_bf16x8(p0[j]));
         else mfma_o(st.o[o - 24][j], a, as_bf16x8(p0[j]));
         if constexpr (o == 31) {
@@ -862,7 +1007,16 @@ __device__ __forceinline__ void video_iter(VideoState<kQT>& st, VideoStream<P>& 
       // ---- this slot's share of the rest ----
       if constexpr (kLazy && (o == 8 || o == 24)) take_max(jc, Const<o == 8 ? 0 : 2>{});
       if constexpr (kLazy && (o == 9 || o == 25)) take_top(jc);
-      if constexpr (j == 1) {
+      if constexpr (P::kQ8) {
+        if constexpr (j == 1) {
+        constexpr int n = o == 1 || o == 2   ? o + 1
+                          : o >= 4 && o < 14 ? o
+                          : o == 17 || o == 18 ? o - 3
+                          : o >= 20 && o < 30 ? o - 4
+                                              : -1;
+        if constexpr (n >= 0 && !(kFirst && n >= 4 && n < 12)) q8_read(Const<(n < 0 ? 0 : n)>{});
+        }
+      } else if constexpr (j == 1) {
         constexpr int n = o + kRingAhead;
         if constexpr (!(kFirst && n >= 8 && n < 16)) st.ring[n & 3] = oread(Const<n>{});
       }
@@ -887,7 +1041,10 @@ __device__ __forceinline__ void video_iter(VideoState<kQT>& st, VideoStream<P>& 
         else if constexpr (o > 28 && (o & 1)) pack_x(Const<k>{}, Const<o - 9>{});
       }
       if constexpr (last) {
-        if constexpr (P::k8) {
+        if constexpr (P::kQ8) {
+          if constexpr (o < 2) stage_codes<o, true>(s, c);
+          else if constexpr (o < 18) stage_word<o + 14, true>(s, c, chunk);
+        } else if constexpr (P::k8) {
           if constexpr (o < 4) {
             stage_word<2 * o, true>(s, c, chunk);
             stage_word<2 * o + 1, true>(s, c, chunk);
@@ -926,7 +1083,7 @@ __device__ __forceinline__ void video_iter(VideoState<kQT>& st, VideoStream<P>& 
 // Finishes the last page of a range (its stage is the one before the
 // stream's current): tile 3's exponentials, then the P*V of chunk 1.
 template <int kQT, class P>
-__device__ __forceinline__ void video_flush(VideoState<kQT>& st, const VideoStream<P>& s) {
+__device__ __forceinline__ void video_flush(VideoState<kQT, P>& st, const VideoStream<P>& s) {
   const uint32_t v1 = s.c.vp;
   mfma_drain();
 #pragma unroll
@@ -961,7 +1118,13 @@ struct VideoSeg {
 
 // How a kernel's queries come: to be normed or scaled, prepared, or as the call says.
 constexpr int kQueriesRaw = 0, kQueriesPrepared = 1, kQueriesAny = 2;
-// A wave's query rows as the call gives them: raw[j][s] = Q[row j][32 s + 8 g .. + 8].
+// First of the 8 dims that word group s of lane group g holds: 32 s + 8 g .., or, against
+// e4m3 codes, s of the 16-dim chunks g and g + 4 (two groups each).
+template <class P>
+__device__ __forceinline__ int query_dim(int s, int g) {
+  return P::kQ8 ? 64 * (s >> 1) + 8 * (s & 1) + 16 * g : 32 * s + 8 * g;
+}
+// A wave's query rows as the call gives them: raw[j][s] = Q[row j][query_dim(s, g) .. + 8].
 template <int kQT>
 struct RawQueries {
   u32x4 raw[kQT][4];
@@ -975,15 +1138,15 @@ __device__ __forceinline__ void fetch_queries(const AttnArgs& a, const VideoSeg&
   const int lane_o = opaque(lane), g = lane_o >> 4, i16 = lane_o & 15;
   // row j's pointer is the first row's plus 16 j token strides (uniform);
   // rows past the end read the zero block (zeros cost the matrix pipe little)
-  const uint16_t* qp = a.q + sg.head * a.q_head_stride + (wrow + i16) * a.q_tok_stride + 8 * g;
+  const uint16_t* qp = a.q + sg.head * a.q_head_stride + (wrow + i16) * a.q_tok_stride + query_dim<P>(0, g);
 #pragma unroll
   for (int j = 0; j < kQT; ++j) {
     const int row = wrow + 16 * j + i16;
     x.ok[j] = row < sg.q_hi;
     x.rider[j] = false;
-    const uint16_t* p = x.ok[j] ? qp + 16 * j * a.q_tok_stride : a.zeros + 8 * g;
+    const uint16_t* p = x.ok[j] ? qp + 16 * j * a.q_tok_stride : a.zeros + query_dim<P>(0, g);
 #pragma unroll
-    for (int s = 0; s < 4; ++s) x.raw[j][s] = *reinterpret_cast<const u32x4*>(p + 32 * s);
+    for (int s = 0; s < 4; ++s) x.raw[j][s] = *reinterpret_cast<const u32x4*>(p + query_dim<P>(s, 0));
     x.pos[j] = make_int3(0, 0, 0);
     if (kQueries != kQueriesPrepared && a.mode == 1 && x.ok[j])
       x.pos[j] = make_int3(a.positions[3 * row], a.positions[3 * row + 1], a.positions[3 * row + 2]);
@@ -1005,8 +1168,8 @@ __device__ __forceinline__ void fetch_queries(const AttnArgs& a, const VideoSeg&
 // The prepared queries, st.q[j][s] = Q''[row j][32 s + 8 g .. + 8], by the
 // call's query mode (2: given as they are, else 0 or 1); rider rows
 // (at and past rq_row0) come prepared.
-template <int kQT, int kQueries>
-__device__ __forceinline__ void prepare_rows(const AttnArgs& a, const RawQueries<kQT>& x, int g, VideoState<kQT>& st) {
+template <int kQT, int kQueries, class P>
+__device__ __forceinline__ void prepare_rows(const AttnArgs& a, const RawQueries<kQT>& x, int g, VideoState<kQT, P>& st) {
   if (kQueries == kQueriesPrepared || (kQueries == kQueriesAny && a.mode == 2)) {
 #pragma unroll
     for (int j = 0; j < kQT; ++j)
@@ -1048,13 +1211,14 @@ __device__ __forceinline__ void prepare_rows(const AttnArgs& a, const RawQueries
   }
 #pragma unroll
   for (int s = 0; s < 4; ++s) {
-    const float4 g0 = *reinterpret_cast<const float4*>(a.gamma + 32 * s + 8 * g);
-    const float4 g1 = *reinterpret_cast<const float4*>(a.gamma + 32 * s + 8 * g + 4);
+    const int d = query_dim<P>(s, g);
+    const float4 g0 = *reinterpret_cast<const float4*>(a.gamma + d);
+    const float4 g1 = *reinterpret_cast<const float4*>(a.gamma + d + 4);
     const float gam[8] = {g0.x, g0.y, g0.z, g0.w, g1.x, g1.y, g1.z, g1.w};
     float2 cs[kQT][4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int p = 16 * s + 4 * g + i;
+      const int p = d / 2 + i;
 #pragma unroll
       for (int j = 0; j < kQT; ++j) cs[j][i] = (p < p0 ? row[j][0] : p < p01 ? row[j][1] : row[j][2])[p];
     }
@@ -1075,14 +1239,48 @@ __device__ __forceinline__ void prepare_rows(const AttnArgs& a, const RawQueries
   }
 }
 
+// e4m3 pages: the rows' two terms and exponents (StateQ8) from their bf16 words.
+template <int kQT, class P>
+__device__ __forceinline__ void split_queries(VideoState<kQT, P>& st) {
+#pragma unroll
+  for (int j = 0; j < kQT; ++j) {
+    float v[32], top = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const uint32_t w = __builtin_bit_cast(u32x4, st.q[j][i >> 2])[i & 3];
+      v[2 * i] = bf16_lo(w);
+      v[2 * i + 1] = bf16_hi(w);
+      top = fmaxf(top, fmaxf(fabsf(v[2 * i]), fabsf(v[2 * i + 1])));
+    }
+    const uint32_t t = __float_as_uint(pair_max<32>(pair_max<16>(top)));
+    // the least f with top <= 448 2^f (448 = 0.875 2^9), for exponent bytes above 0
+    const int f = max(static_cast<int>(t >> 23) - 135 + ((t & 0x7fffffu) > 0x600000u ? 1 : 0), -122);
+    const float inv = __uint_as_float(static_cast<uint32_t>(127 - f) << 23);
+    st.q_exp[j] = (f + 127) | ((f + 123) << 8);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float x[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[k] = v[4 * i + k] * inv;
+      int c1 = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false);
+      c1 = __builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], c1, true);
+      const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(c1, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(c1, true);
+      int c2 = __builtin_amdgcn_cvt_pk_fp8_f32((x[0] - lo[0]) * 16.f, (x[1] - lo[1]) * 16.f, 0, false);
+      c2 = __builtin_amdgcn_cvt_pk_fp8_f32((x[2] - hi[0]) * 16.f, (x[3] - hi[1]) * 16.f, c2, true);
+      st.q8[j][0][i] = c1;
+      st.q8[j][1][i] = c2;
+    }
+  }
+}
+
 template <int kQT, int kQueries, class P>
 __device__ __forceinline__ void video_segment(const AttnArgs& a, const VideoSeg& sg, VideoStream<P>& s, int wave) {
   const int wrow = sg.q_lo + wave * 16 * kQT;
-  VideoState<kQT> st;
+  VideoState<kQT, P> st;
   {
     RawQueries<kQT> raw;
     fetch_queries<kQT, kQueries, P>(a, sg, wrow, s.lane, raw);
-    prepare_rows<kQT, kQueries>(a, raw, s.lane >> 4, st);
+    prepare_rows<kQT, kQueries, P>(a, raw, s.lane >> 4, st);
   }
 
   // ---- softmax shift ----
@@ -1117,6 +1315,7 @@ __device__ __forceinline__ void video_segment(const AttnArgs& a, const VideoSeg&
     const float neg = is ? 0.f : -bound;
     st.s_init[j] = (f32x4){neg, neg, neg, neg};
   }
+  if constexpr (P::kQ8) split_queries(st);
   st.any_lazy = __any(lazy);
   if constexpr (P::kWin) {
     st.any_unset = st.any_lazy;
@@ -1522,9 +1721,9 @@ __device__ __forceinline__ void video_idle_segment(const AttnArgs& a, const Vide
       s.at += 1;
       s.stage = ring_add(s.stage, 1);
       if constexpr (P::k8) {
-        s.c.ks = s.c.ks_load;
+        if constexpr (!P::kQ8) s.c.ks = s.c.ks_load;
         s.c.vs = s.c.vs_load;
-        s.c.ks_load = peek_lanes(s.ks, at);
+        if constexpr (!P::kQ8) s.c.ks_load = peek_lanes(s.ks, at);
         s.c.vs_load = peek_lanes(s.vs, at);
         s.c.wk = s.wk + ring_add(s.stage, 2);
         s.c.wv = s.wv + ring_add(s.stage, 2);
@@ -1725,17 +1924,23 @@ __device__ __forceinline__ void unit_attn(const AttnArgs& a) {
     s.dma_v = 2 * v_tile_index(8 * ((lane & 7) ^ ((d >> 1) & 7)), d);
     const uint32_t lds = lds_offset(g_stages);
     if constexpr (P::k8) {
-      const uint32_t t = 64u * wave + lane, key = t >> 2, part = t & 3;
-      // K: row 16 tile + m of the key, chunks 2 part (and 8 further, and the odd ones)
+      // A write takes 8 lanes at a time, over 128 bytes of banks: eight neighbours hold
+      // two keys that are two apart, whose rows' swizzles send their chunks to even and
+      // odd positions (e4m3 K: to the low and high ones).
+      const uint32_t n = 64u * wave + lane, key = swap_low_bits(n >> 2), part = n & 3, t = 4 * key + part;
       const uint32_t tile = 2 * (key >> 5) + ((key >> 2) & 1), row = 4 * ((key >> 3) & 3) + (key & 3);
       s.load[0] = 16u * t;
       s.load[1] = opaque(16u * t + 4096u);  // (a register of its own: an offset beside a scalar base)
-      s.wk = lds + 256u * (16u * tile + row) + 16u * ((2u * part) ^ row);
+      // K: row 16 tile + m of the key, chunks 2 part (and 8 further, and the odd ones)
+      s.wk = P::kQ8 ? lds + 128u * (16u * tile + row) + 16u * (part ^ codes_swizzle(row))
+                    : lds + 256u * (16u * tile + row) + 16u * ((2u * part) ^ swap_low_bits(row));
       s.wv = lds + kStageV + 128u * key + 16u * ((2u * part) ^ ((key >> 1) & 7));  // (V^T: dim t / 4)
     }
     s.lds0 = __builtin_amdgcn_readfirstlane(lds + 1024u * wave);
     const int g = lane >> 4, i16 = lane & 15;
-    s.k_read = lds + 256u * i16 + 16u * (g ^ i16);
+    s.k_read = P::kQ8  ? lds + 128u * i16 + 16u * (g ^ codes_swizzle(i16))
+               : P::k8 ? lds + 256u * i16 + 16u * (g ^ swap_low_bits(i16))
+                       : lds + 256u * i16 + 16u * (g ^ i16);
     s.v_read = lds + kStageV + 128u * i16 + 16u * (g ^ ((i16 >> 1) & 7));
   }
   const bool rx = P::kPlain && a.rx_pages > 0 && qt == n_qtiles - 1 && wave == kVideoWaves - 1;
