@@ -429,20 +429,26 @@ __device__ __forceinline__ void stage_codes(VideoStream<P>& s, const PageCtx<P>&
   *(__attribute__((address_space(3))) u32x4*)(c.wk ^ (64u * kPart)) = s.raw[kPart];
   if constexpr (kAgain) load_part<kPart>(s, c);
 }
-template <int kWord, bool kAgain, class P>
-__device__ __forceinline__ void stage_word(VideoStream<P>& s, const PageCtx<P>& c, u32x4& chunk) {
-  constexpr int part = kWord >> 3, h = (kWord >> 2) & 1;
+template <int kWord, class P>
+__device__ __forceinline__ void convert_word(const VideoStream<P>& s, const PageCtx<P>& c, u32x4& chunk) {
+  constexpr int part = kWord >> 3;
   uint32_t scale = part < 2 ? c.ks : c.vs;
   if constexpr (P::kQ8) scale &= 0xff800000u;
-  const QuantScale q = quant_scale<P::kFmt>(__uint_as_float(scale));
-  uint32_t w = codes_to_bf16<P::kFmt, kWord & 1>(s.raw[part][(kWord & 7) >> 1], q);
+  uint32_t w = codes_to_bf16<P::kFmt, kWord & 1>(s.raw[part][(kWord & 7) >> 1], quant_scale<P::kFmt>(__uint_as_float(scale)));
   asm volatile("" : "+v"(w));
   chunk[kWord & 3] = w;
-  if constexpr ((kWord & 3) == 3) {
-    const uint32_t at = part < 2 ? (c.wk ^ (16u * h) ^ (128u * (part & 1))) : (c.wv ^ (16u * h)) + 8192u * (part & 1);
-    *(__attribute__((address_space(3))) u32x4*)at = chunk;
-  }
-  if constexpr (kAgain && (kWord & 7) == 7) load_part<part>(s, c);
+}
+template <int kChunk, class P>
+__device__ __forceinline__ void write_chunk(const PageCtx<P>& c, const u32x4& chunk) {
+  constexpr int part = kChunk >> 1, h = kChunk & 1;
+  const uint32_t at = part < 2 ? (c.wk ^ (16u * h) ^ (128u * (part & 1))) : (c.wv ^ (16u * h)) + 8192u * (part & 1);
+  *(__attribute__((address_space(3))) u32x4*)at = chunk;
+}
+template <int kWord, bool kAgain, class P>
+__device__ __forceinline__ void stage_word(VideoStream<P>& s, const PageCtx<P>& c, u32x4& chunk) {
+  convert_word<kWord>(s, c, chunk);
+  if constexpr ((kWord & 3) == 3) write_chunk<(kWord >> 2)>(c, chunk);
+  if constexpr (kAgain && (kWord & 7) == 7) load_part<(kWord >> 3)>(s, c);
 }
 template <bool kAgain, class P>
 __device__ __forceinline__ void stage_page(VideoStream<P>& s, const PageCtx<P>& c) {
@@ -455,9 +461,11 @@ __device__ __forceinline__ void stage_page(VideoStream<P>& s, const PageCtx<P>& 
     stage_word<decltype(n)::value + (P::kQ8 ? 16 : 0), kAgain>(s, c, chunk);
   });
 }
-// Waits for the wave's LDS accesses, all or all but the last three.
+// Waits for the wave's LDS accesses, all or all but the operand reads that run ahead
+// into the next page (three, e4m3 four).
 __device__ __forceinline__ void wait_lds() { __builtin_amdgcn_s_waitcnt(0xC07F); }
-__device__ __forceinline__ void wait_lds_but_3() { __builtin_amdgcn_s_waitcnt(0xC37F); }
+template <class P>
+__device__ __forceinline__ void wait_lds_but_ahead() { __builtin_amdgcn_s_waitcnt(P::kQ8 ? 0xC47F : 0xC37F); }
 
 // Waits for this wave's direct loads of every page but the one issued last
 // (loads retire in order).  The barrier that follows then makes every wave's
@@ -681,7 +689,10 @@ __device__ __forceinline__ void video_iter(VideoState<kQT, P>& st, VideoStream<P
   const PageCtx<P> c = s.c;
   const bool tail = P::kWin ? n_valid != kPageTokens : n_valid < kPageTokens;
   PageCtx<P> nx;
-  [[maybe_unused]] u32x4 chunk;
+  [[maybe_unused]] u32x4 chunk[P::kQ8 ? 4 : 1];
+  // (redefined every page, or the compiler widens them to pairs outside the loop and adds
+  // the loads' scalar base to those)
+  if constexpr (P::k8) asm volatile("" : "+v"(s.load[0]), "+v"(s.load[1]));
   pin_queries(st);
   pin_v(st.ones);
   page_barrier();
@@ -695,14 +706,15 @@ __device__ __forceinline__ void video_iter(VideoState<kQT, P>& st, VideoStream<P
     else return lds_read16(c.v + 2048u * (n - 24));
   };
   // e4m3: read n of a page's 24 (K tiles 0 and 1 two each, V^T chunk 1 of the page
-  // before eight, K tiles 2 and 3, V^T chunk 0; 24 and 25 are the next page's first),
-  // into slot n % 6; the read that step o issues is three or four steps ahead of its
-  // use and behind the last use of the slot's former one
+  // before eight, K tiles 2 and 3, V^T chunk 0; 24 to 27 are the next page's first), into
+  // slot n % 6.  Steps 4-15 issue reads 4-15, steps 20-31 reads 16-27, each three steps or
+  // more ahead of its use and behind the last use of the slot's former one; the steps
+  // between them issue the writes.
   [[maybe_unused]] auto q8_read = [&](auto nc) __attribute__((always_inline)) {
     constexpr int n = decltype(nc)::value, slot = n % 6;
     if constexpr (P::kQ8) {
       uint32_t at;
-      if constexpr (n >= 24) at = nx.k[n - 24];
+      if constexpr (n >= 24) at = nx.k[n & 1] + 2048u * ((n - 24) >> 1);
       else if constexpr (n >= 16) at = c.v + 2048u * (n - 16);
       else if constexpr (n >= 12) at = c.k[n & 1] + 2048u * (2 + ((n - 12) >> 1));
       else if constexpr (n >= 4) at = c.vp + 2048u * (n - 4);
@@ -737,8 +749,7 @@ __device__ __forceinline__ void video_iter(VideoState<kQT, P>& st, VideoStream<P
   };
   if constexpr (kFirst) {
     if constexpr (P::kQ8) {
-      q8_read(Const<0>{});
-      q8_read(Const<1>{});
+      static_for<4>(q8_read);
     } else {
       static_for<kRingAhead>([&](auto n) __attribute__((always_inline)) { st.ring[decltype(n)::value] = oread(n); });
     }
@@ -921,7 +932,7 @@ __device__ __forceinline__ void video_iter(VideoState<kQT, P>& st, VideoStream<P
     }
     if constexpr (o == 15) { st_next = ring_add(s.stage, 1); pin_s(st_next); }
     constexpr uint32_t tile_shift = P::k8 ? kCodeTileShift : 14;
-    constexpr int ld_step = P::k8 ? 28 : 16;
+    constexpr int ld_step = P::kQ8 ? 30 : P::k8 ? 28 : 16, vs_step = P::kQ8 ? 28 : 26;
     if constexpr (o == ld_step) {
       nx.ldk = reinterpret_cast<const uint16_t*>(reinterpret_cast<uint64_t>(s.kpool) + (static_cast<uint64_t>(ent >> 7) << tile_shift));
       pin_s(nx.ldk);
@@ -946,24 +957,24 @@ __device__ __forceinline__ void video_iter(VideoState<kQT, P>& st, VideoStream<P
         nx.ks_load = (look & 64) ? w1 : nx.ks_load;
         pin_s(nx.ks_load);
       }
-      if constexpr (o == 26) { nx.vs_load = __builtin_amdgcn_readlane(s.vs[0], look & 63); pin_s(nx.vs_load); }
-      if constexpr (o == 27) {
+      if constexpr (o == vs_step) { nx.vs_load = __builtin_amdgcn_readlane(s.vs[0], look & 63); pin_s(nx.vs_load); }
+      if constexpr (o == vs_step + 1) {
         const uint32_t w1 = __builtin_amdgcn_readlane(s.vs[1], look & 63);
         nx.vs_load = (look & 64) ? w1 : nx.vs_load;
         pin_s(nx.vs_load);
       }
-      if constexpr (o == 18) { nx.wk = s.wk + ring_add(st_next, 2); pin_v(nx.wk); }
-      if constexpr (o == 19) { nx.wv = s.wv + ring_add(st_next, 2); pin_v(nx.wv); }
+      if constexpr (o == (P::kQ8 ? 24 : 18)) { nx.wk = s.wk + ring_add(st_next, 2); pin_v(nx.wk); }
+      if constexpr (o == (P::kQ8 ? 25 : 19)) { nx.wv = s.wv + ring_add(st_next, 2); pin_v(nx.wv); }
     } else {
       if constexpr (o == 18) { nx.lds = s.lds0 + ring_add(st_next, 3); pin_s(nx.lds); }
     }
-    if constexpr (o == 19) { nx.k[0] = s.k_read + st_next; pin_v(nx.k[0]); }
-    if constexpr (o == 20) { nx.k[1] = nx.k[0] ^ 64u; pin_v(nx.k[1]); }
+    if constexpr (o == (P::kQ8 ? 24 : 19)) { nx.k[0] = s.k_read + st_next; pin_v(nx.k[0]); }
+    if constexpr (o == (P::kQ8 ? 25 : 20)) { nx.k[1] = nx.k[0] ^ 64u; pin_v(nx.k[1]); }
     if constexpr (o == 21 && !P::kQ8) { nx.k[2] = nx.k[0] ^ 128u; pin_v(nx.k[2]); }
     if constexpr (o == 22 && !P::kQ8) { nx.k[3] = nx.k[0] ^ 192u; pin_v(nx.k[3]); }
-    if constexpr (o == 23) { nx.v = s.v_read + st_next; pin_v(nx.v); }
-    if constexpr (o == 24) { nx.vp = c.v ^ 64u; pin_v(nx.vp); }
-    if constexpr (o == 28) { s.valid = __builtin_amdgcn_readfirstlane((s.valid >> 8) | ((ent & 127u) << 24)); }
+    if constexpr (o == (P::kQ8 ? 30 : 23)) { nx.v = s.v_read + st_next; pin_v(nx.v); }
+    if constexpr (o == (P::kQ8 ? 14 : 24)) { nx.vp = c.v ^ 64u; pin_v(nx.vp); }
+    if constexpr (o == (P::kQ8 ? 31 : 28)) { s.valid = __builtin_amdgcn_readfirstlane((s.valid >> 8) | ((ent & 127u) << 24)); }
   };
   static_for<32>([&](auto oc) __attribute__((always_inline)) {
     constexpr int o = decltype(oc)::value;
@@ -980,7 +991,7 @@ __device__ __forceinline__ void video_iter(VideoState<kQT, P>& st, VideoStream<P
           if constexpr (slot % 2 == 0) {
             mfma_s8<term>(sa[t][jj], st.pair[t & 1], st.q8[jj][term], term == 0 ? st.s_init[jj] : sa[t][jj],
                           static_cast<int>(c.k_exp), st.q_exp[jj]);
-            pin_v(sa[t][jj]);
+            if constexpr (term == 1) pin_v(sa[t][jj]);
           }
         } else {
           const bf16x8 a = st.ring[o & 3];
@@ -1008,17 +1019,20 @@ __device__ __forceinline__ void video_iter(VideoState<kQT, P>& st, VideoStream<P
       if constexpr (kLazy && (o == 8 || o == 24)) take_max(jc, Const<o == 8 ? 0 : 2>{});
       if constexpr (kLazy && (o == 9 || o == 25)) take_top(jc);
       if constexpr (P::kQ8) {
-        if constexpr (j == 1) {
-        constexpr int n = o == 1 || o == 2   ? o + 1
-                          : o >= 4 && o < 14 ? o
-                          : o == 17 || o == 18 ? o - 3
-                          : o >= 20 && o < 30 ? o - 4
-                                              : -1;
-        if constexpr (n >= 0 && !(kFirst && n >= 4 && n < 12)) q8_read(Const<(n < 0 ? 0 : n)>{});
-        }
+        constexpr int n = (o & 15) < 4 ? -1 : o < 16 ? o : o - 4;
+        if constexpr (j == 1 && n >= 0 && !(kFirst && n < 12)) q8_read(Const<(n < 0 ? 0 : n)>{});
       } else if constexpr (j == 1) {
         constexpr int n = o + kRingAhead;
         if constexpr (!(kFirst && n >= 8 && n < 16)) st.ring[n & 3] = oread(Const<n>{});
+      }
+      if constexpr (P::kQ8 && (o == 8 || o == 9)) {
+        // V's conversions, where there are no exponentials
+        constexpr int slot = (o - 8) * kQT + j, w0 = 8 * slot / kQT, w1 = 8 * (slot + 1) / kQT;
+        static_for<w1 - w0>([&](auto n) __attribute__((always_inline)) {
+          constexpr int word = 16 + w0 + decltype(n)::value;
+          convert_word<word>(s, c, chunk[(word - 16) >> 2]);
+          if constexpr ((word & 7) == 7) load_part<(word >> 3)>(s, c);
+        });
       }
       if constexpr (even) {
         if constexpr (o < 8) exp_x(Const<k>{}, Const<24 + o>{});
@@ -1042,14 +1056,15 @@ __device__ __forceinline__ void video_iter(VideoState<kQT, P>& st, VideoStream<P
       }
       if constexpr (last) {
         if constexpr (P::kQ8) {
-          if constexpr (o < 2) stage_codes<o, true>(s, c);
-          else if constexpr (o < 18) stage_word<o + 14, true>(s, c, chunk);
+          // the LDS writes: in steps that read no operand
+          if constexpr (o == 0 || o == 2) stage_codes<o / 2, true>(s, c);
+          if constexpr (o >= 16 && o < 20) write_chunk<o - 12>(c, chunk[o - 16]);
         } else if constexpr (P::k8) {
           if constexpr (o < 4) {
-            stage_word<2 * o, true>(s, c, chunk);
-            stage_word<2 * o + 1, true>(s, c, chunk);
+            stage_word<2 * o, true>(s, c, chunk[0]);
+            stage_word<2 * o + 1, true>(s, c, chunk[0]);
           } else if constexpr (o < 28) {
-            stage_word<o + 4, true>(s, c, chunk);
+            stage_word<o + 4, true>(s, c, chunk[0]);
           }
         } else if constexpr (o < kDmaPerPage) {
           issue_load<o>(s, c);
@@ -1071,7 +1086,7 @@ __device__ __forceinline__ void video_iter(VideoState<kQT, P>& st, VideoStream<P
   // After a range's first page everything is waited for: a load the compiler
   // knows of and believes in flight on entry to the page loop would be waited
   // for in every iteration, with all the direct loads behind it.
-  if constexpr (P::k8) wait_lds_but_3();
+  if constexpr (P::k8) wait_lds_but_ahead<P>();
   else if constexpr (kFirst) wait_dma_all();
   else wait_dma_all_but_last_page();
   s.c = nx;
