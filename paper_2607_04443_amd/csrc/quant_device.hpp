@@ -23,14 +23,21 @@ template <int kFmt>
 __device__ __forceinline__ QuantScale quant_scale(float s) {
   return QuantScale{s, kFmt == kFmtInt8 ? -1152.0f * s : 0.f};
 }
+template <int kHalf>
+__device__ __forceinline__ uint32_t spread_codes(uint32_t codes) {
+  return __builtin_amdgcn_perm(0x64646464u, codes, kHalf ? 0x04030402u : 0x04010400u);
+}
+template <int kHalf>
+__device__ __forceinline__ float spread_value(uint32_t p, const QuantScale& q) {
+  return fmaf(static_cast<float>(__builtin_bit_cast(f16x2, p)[kHalf]), q.s, q.c);
+}
 template <int kFmt, int kHalf>
 __device__ __forceinline__ uint32_t codes_to_bf16(uint32_t codes, const QuantScale& q) {
   if constexpr (kFmt == kFmtE4m3) {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, q.s, kHalf == 1));
   } else {
-    const uint32_t p = __builtin_amdgcn_perm(0x64646464u, codes, kHalf ? 0x04030402u : 0x04010400u);
-    const f16x2 h = __builtin_bit_cast(f16x2, p);
-    return pack_bf16(fmaf(static_cast<float>(h[0]), q.s, q.c), fmaf(static_cast<float>(h[1]), q.s, q.c));
+    const uint32_t p = spread_codes<kHalf>(codes);
+    return pack_bf16(spread_value<0>(p, q), spread_value<1>(p, q));
   }
 }
 // Eight codes (two words) as an MFMA operand.

@@ -51,6 +51,7 @@ struct Path {
   static constexpr bool k8 = kFormat != kFmtBf16;
   static constexpr bool kWin = kWindow;
   static constexpr bool kPlain = kFormat == kFmtBf16 && !kWindow;
+  static constexpr bool kPieces = kFormat == kFmtInt8;  // conversions an instruction at a time
   static constexpr bool kQ8 = kFormat == kFmtE4m3;  // S by 8-bit products (VideoState)
 };
 using PlainPath = Path<kFmtBf16, false>;
@@ -438,6 +439,47 @@ __device__ __forceinline__ void convert_word(const VideoStream<P>& s, const Page
   asm volatile("" : "+v"(w));
   chunk[kWord & 3] = w;
 }
+// int8: the same an instruction at a time, in the order
+//   spread word w, high value of w - 1 | pack w - 1, low value of w | ...
+// which leaves an instruction between a mixed fma and what reads it (else a wait state):
+// piece 2 w of 66 is the first pair, piece 2 w + 1 the second.
+struct WordPieces {
+  uint32_t u;
+  float lo, hi;
+};
+template <int kPiece, class P>
+__device__ __forceinline__ void convert_piece(VideoStream<P>& s, const PageCtx<P>& c, WordPieces& x, u32x4& chunk) {
+  constexpr int word = kPiece >> 1, part = word >> 3, part_before = (word - 1) >> 3;
+  const QuantScale qk = quant_scale<P::kFmt>(__uint_as_float(c.ks)), qv = quant_scale<P::kFmt>(__uint_as_float(c.vs));
+  if constexpr ((kPiece & 1) == 0) {
+    if constexpr (word > 0) x.hi = spread_value<1>(x.u, part_before < 2 ? qk : qv);
+    if constexpr (word < 32) x.u = spread_codes<word & 1>(s.raw[part][(word & 7) >> 1]);
+  } else {
+    const float lo = x.lo;
+    if constexpr (word < 32) x.lo = spread_value<0>(x.u, part < 2 ? qk : qv);
+    if constexpr (word > 0) {
+      uint32_t w = pack_bf16(lo, x.hi);
+      asm volatile("" : "+v"(w));
+      chunk[(word - 1) & 3] = w;
+      if constexpr ((word & 3) == 0) write_chunk<(word >> 2) - 1>(c, chunk);
+    }
+  }
+}
+// What follows pieces kFrom .. kTo - 1 in their slot: their values stay in it, a part
+// whose codes are all spread is loaded again.
+template <int kFrom, int kTo, class P>
+__device__ __forceinline__ void end_pieces(VideoStream<P>& s, const PageCtx<P>& c, WordPieces& x) {
+  static_for<kTo - kFrom>([&](auto n) __attribute__((always_inline)) {
+    constexpr int piece = kFrom + decltype(n)::value, word = piece >> 1;
+    if constexpr ((piece & 1) == 0) {
+      if constexpr (word > 0 && piece + 1 == kTo) asm volatile("" : "+v"(x.hi));
+      if constexpr (word < 32 && piece + 1 == kTo) asm volatile("" : "+v"(x.u));
+      if constexpr (word < 32 && (word & 7) == 7) load_part<(word >> 3)>(s, c);
+    } else {
+      if constexpr (word < 32 && piece + 1 == kTo) asm volatile("" : "+v"(x.lo));
+    }
+  });
+}
 template <int kChunk, class P>
 __device__ __forceinline__ void write_chunk(const PageCtx<P>& c, const u32x4& chunk) {
   constexpr int part = kChunk >> 1, h = kChunk & 1;
@@ -677,10 +719,14 @@ __device__ __forceinline__ void scale_raised(VideoState<kQT, P>& st) {
 // the largest weight, and out of its reach, from 5 on, the range ran unpipelined
 // under a running maximum: 344 to 455.)
 //
-// 8-bit pages: beside them, a word of bf16 per step (two in the first four; stage_word)
-// turns the codes of page p + 2 into its stage, steps 0-27; the operand reads of
-// steps 28-31 follow the last write, so a wait for all but the wave's last three LDS
-// accesses ends the page.
+// 8-bit pages: beside them the codes of page p + 2, in registers since the page before,
+// are turned into its stage and those of page p + 3 requested.  int8: 128 instructions
+// of conversion (WordPieces), in the slots without exponentials; they fill more than
+// those have room for (517 instructions a page, 378 of bf16 pages), which costs the
+// int8 kernel a fifth over bf16.  A word per step at its end took 5% longer.  e4m3: 16
+// conversions of V^T in steps 8 and 9, the writes in the steps that read no operand.
+// The operand reads that run ahead into the next page follow the last write, so a wait
+// for all but those ends the page.
 // Windows: what hides keys is a page's edge flag, the wave's own.  A row may meet
 // its first visible key late: until then its m is unset and its S the bare logits.
 template <int kQT, bool kFirst, bool kLazy, class P>
@@ -690,6 +736,7 @@ __device__ __forceinline__ void video_iter(VideoState<kQT, P>& st, VideoStream<P
   const bool tail = P::kWin ? n_valid != kPageTokens : n_valid < kPageTokens;
   PageCtx<P> nx;
   [[maybe_unused]] u32x4 chunk[P::kQ8 ? 4 : 1];
+  [[maybe_unused]] WordPieces pieces;
   // (redefined every page, or the compiler widens them to pairs outside the loop and adds
   // the loads' scalar base to those)
   if constexpr (P::k8) asm volatile("" : "+v"(s.load[0]), "+v"(s.load[1]));
@@ -921,28 +968,31 @@ __device__ __forceinline__ void video_iter(VideoState<kQT, P>& st, VideoStream<P
   // the next page's context, one small piece per step
   int look = 0;
   uint32_t ent = 0, st_next = 0;
+  // (at: the steps that take the pieces, by path.  8-bit paths keep them out of the
+  // steps that conversions and 8-bit products fill; steps 32 + o are int8's second
+  // place in step o)
   auto next_ctx = [&](auto oc) __attribute__((always_inline)) {
     constexpr int o = decltype(oc)::value;
-    if constexpr (o == 12) { look = min(s.at + 4, s.n - 1); pin_s(look); }
-    if constexpr (o == 13) { ent = __builtin_amdgcn_readlane(s.ent[0], look & 63); pin_s(ent); }
-    if constexpr (o == 14) {
+    constexpr auto at = [](int plain, int e4m3, int int8) { return o == (P::kPieces ? int8 : P::kQ8 ? e4m3 : plain); };
+    if constexpr (at(12, 12, 10)) { look = min(s.at + 4, s.n - 1); pin_s(look); }
+    if constexpr (at(13, 13, 11)) { ent = __builtin_amdgcn_readlane(s.ent[0], look & 63); pin_s(ent); }
+    if constexpr (at(14, 14, 32 + 26)) {
       const uint32_t e1 = __builtin_amdgcn_readlane(s.ent[1], look & 63);
       ent = (look & 64) ? e1 : ent;
       pin_s(ent);
     }
-    if constexpr (o == 15) { st_next = ring_add(s.stage, 1); pin_s(st_next); }
+    if constexpr (at(15, 15, 26)) { st_next = ring_add(s.stage, 1); pin_s(st_next); }
     constexpr uint32_t tile_shift = P::k8 ? kCodeTileShift : 14;
-    constexpr int ld_step = P::kQ8 ? 30 : P::k8 ? 28 : 16, vs_step = P::kQ8 ? 28 : 26;
-    if constexpr (o == ld_step) {
+    if constexpr (at(16, 30, 32 + 31)) {
       nx.ldk = reinterpret_cast<const uint16_t*>(reinterpret_cast<uint64_t>(s.kpool) + (static_cast<uint64_t>(ent >> 7) << tile_shift));
       pin_s(nx.ldk);
     }
-    if constexpr (o == ld_step + 1) {
+    if constexpr (at(17, 31, 31)) {
       nx.ldv = reinterpret_cast<const uint16_t*>(reinterpret_cast<uint64_t>(s.vpool) + (static_cast<uint64_t>(ent >> 7) << tile_shift));
       pin_s(nx.ldv);
     }
     if constexpr (P::k8) {
-      if constexpr (o == 15) {
+      if constexpr (at(-1, 15, 26)) {
         if constexpr (P::kQ8) {
           nx.k_exp = c.vs1;
           nx.vs1 = c.vs;
@@ -951,36 +1001,37 @@ __device__ __forceinline__ void video_iter(VideoState<kQT, P>& st, VideoStream<P
         }
         nx.vs = c.vs_load;
       }
-      if constexpr (o == 24 && !P::kQ8) { nx.ks_load = __builtin_amdgcn_readlane(s.ks[0], look & 63); pin_s(nx.ks_load); }
-      if constexpr (o == 25 && !P::kQ8) {
+      if constexpr (at(-1, -1, 32 + 28)) { nx.ks_load = __builtin_amdgcn_readlane(s.ks[0], look & 63); pin_s(nx.ks_load); }
+      if constexpr (at(-1, -1, 28)) {
         const uint32_t w1 = __builtin_amdgcn_readlane(s.ks[1], look & 63);
         nx.ks_load = (look & 64) ? w1 : nx.ks_load;
         pin_s(nx.ks_load);
       }
-      if constexpr (o == vs_step) { nx.vs_load = __builtin_amdgcn_readlane(s.vs[0], look & 63); pin_s(nx.vs_load); }
-      if constexpr (o == vs_step + 1) {
+      if constexpr (at(-1, 28, 32 + 29)) { nx.vs_load = __builtin_amdgcn_readlane(s.vs[0], look & 63); pin_s(nx.vs_load); }
+      if constexpr (at(-1, 29, 29)) {
         const uint32_t w1 = __builtin_amdgcn_readlane(s.vs[1], look & 63);
         nx.vs_load = (look & 64) ? w1 : nx.vs_load;
         pin_s(nx.vs_load);
       }
-      if constexpr (o == (P::kQ8 ? 24 : 18)) { nx.wk = s.wk + ring_add(st_next, 2); pin_v(nx.wk); }
-      if constexpr (o == (P::kQ8 ? 25 : 19)) { nx.wv = s.wv + ring_add(st_next, 2); pin_v(nx.wv); }
+      if constexpr (at(-1, 24, 30)) { nx.wk = s.wk + ring_add(st_next, 2); pin_v(nx.wk); }
+      if constexpr (at(-1, 25, 30)) { nx.wv = s.wv + ring_add(st_next, 2); pin_v(nx.wv); }
     } else {
       if constexpr (o == 18) { nx.lds = s.lds0 + ring_add(st_next, 3); pin_s(nx.lds); }
     }
-    if constexpr (o == (P::kQ8 ? 24 : 19)) { nx.k[0] = s.k_read + st_next; pin_v(nx.k[0]); }
-    if constexpr (o == (P::kQ8 ? 25 : 20)) { nx.k[1] = nx.k[0] ^ 64u; pin_v(nx.k[1]); }
-    if constexpr (o == 21 && !P::kQ8) { nx.k[2] = nx.k[0] ^ 128u; pin_v(nx.k[2]); }
-    if constexpr (o == 22 && !P::kQ8) { nx.k[3] = nx.k[0] ^ 192u; pin_v(nx.k[3]); }
-    if constexpr (o == (P::kQ8 ? 30 : 23)) { nx.v = s.v_read + st_next; pin_v(nx.v); }
-    if constexpr (o == (P::kQ8 ? 14 : 24)) { nx.vp = c.v ^ 64u; pin_v(nx.vp); }
-    if constexpr (o == (P::kQ8 ? 31 : 28)) { s.valid = __builtin_amdgcn_readfirstlane((s.valid >> 8) | ((ent & 127u) << 24)); }
+    if constexpr (at(19, 24, 27)) { nx.k[0] = s.k_read + st_next; pin_v(nx.k[0]); }
+    if constexpr (at(20, 25, 32 + 28)) { nx.k[1] = nx.k[0] ^ 64u; pin_v(nx.k[1]); }
+    if constexpr (at(21, -1, 32 + 30)) { nx.k[2] = nx.k[0] ^ 128u; pin_v(nx.k[2]); }
+    if constexpr (at(22, -1, 32 + 30)) { nx.k[3] = nx.k[0] ^ 192u; pin_v(nx.k[3]); }
+    if constexpr (at(23, 30, 31)) { nx.v = s.v_read + st_next; pin_v(nx.v); }
+    if constexpr (at(24, 14, 14)) { nx.vp = c.v ^ 64u; pin_v(nx.vp); }
+    if constexpr (at(28, 31, 31)) { s.valid = __builtin_amdgcn_readfirstlane((s.valid >> 8) | ((ent & 127u) << 24)); }
   };
   static_for<32>([&](auto oc) __attribute__((always_inline)) {
     constexpr int o = decltype(oc)::value;
     static_for<kQT>([&](auto jc) __attribute__((always_inline)) {
       constexpr int j = decltype(jc)::value, k = j >> 1;
       constexpr bool even = (j & 1) == 0, last = j == kQT - 1;
+      [[maybe_unused]] constexpr int last_odd = kQT == 4 ? 3 : kQT - 1;
       // ---- the MFMA ----
       constexpr bool s_step = o < 8 || (o >= 16 && o < 24);
       if constexpr (s_step) {
@@ -1034,6 +1085,17 @@ __device__ __forceinline__ void video_iter(VideoState<kQT, P>& st, VideoStream<P
           if constexpr ((word & 7) == 7) load_part<(word >> 3)>(s, c);
         });
       }
+      // int8: 66 pieces, one in each odd slot of a step with exponentials in the even ones,
+      // six and seven in the steps without any
+      constexpr bool many = o == 8 || o == 9 || o == 24 || o == 25, one = o < 8 || (o >= 12 && o < 24);
+      constexpr int first = o < 8 ? 2 * o : o < 10 ? 16 + 6 * (o - 8) : o < 24 ? 28 + 2 * (o - 12) : 52 + 7 * (o - 24);
+      constexpr int n_step = o < 10 ? 6 : 7;
+      constexpr int piece0 = first + (many ? n_step * j / kQT : one ? (j == 0 ? 0 : j == 1 ? 0 : j == last_odd ? 1 : 2) : 0);
+      constexpr int piece1 = first + (many ? n_step * (j + 1) / kQT : one ? (j == 0 ? 0 : j == last_odd ? 2 : j == 1 ? 1 : 2) : 0);
+      if constexpr (P::kPieces)
+        static_for<piece1 - piece0>([&](auto n) __attribute__((always_inline)) {
+          convert_piece<piece0 + decltype(n)::value>(s, c, pieces, chunk[0]);
+        });
       if constexpr (even) {
         if constexpr (o < 8) exp_x(Const<k>{}, Const<24 + o>{});
         else if constexpr (o == 10) exp_x(Const<k>{}, Const<0>{});
@@ -1054,24 +1116,19 @@ __device__ __forceinline__ void video_iter(VideoState<kQT, P>& st, VideoStream<P
         else if constexpr (o == 28) pack_x(Const<k>{}, Const<18>{});
         else if constexpr (o > 28 && (o & 1)) pack_x(Const<k>{}, Const<o - 9>{});
       }
+      if constexpr (P::kPieces && j == 1) next_ctx(Const<32 + o>{});  // (before the last slot's)
       if constexpr (last) {
         if constexpr (P::kQ8) {
           // the LDS writes: in steps that read no operand
           if constexpr (o == 0 || o == 2) stage_codes<o / 2, true>(s, c);
           if constexpr (o >= 16 && o < 20) write_chunk<o - 12>(c, chunk[o - 16]);
-        } else if constexpr (P::k8) {
-          if constexpr (o < 4) {
-            stage_word<2 * o, true>(s, c, chunk[0]);
-            stage_word<2 * o + 1, true>(s, c, chunk[0]);
-          } else if constexpr (o < 28) {
-            stage_word<o + 4, true>(s, c, chunk[0]);
-          }
-        } else if constexpr (o < kDmaPerPage) {
+        } else if constexpr (!P::k8 && o < kDmaPerPage) {
           issue_load<o>(s, c);
         }
         next_ctx(oc);
         if constexpr (o == 14 || o == 30) pin_v(st.ones);
       }
+      if constexpr (P::kPieces) end_pieces<piece0, piece1>(s, c, pieces);
       sched_fence();
     });
     if constexpr (o == 9) check_chunk(Const<0>{});
