@@ -110,7 +110,8 @@ typedef struct ws_cache_config {
  * Keys are normed and rotated in fp32 and rounded once, to the code.  An
  * infinity, a NaN and, for INT8, a magnitude of 2^118 or more is stored as 0 and
  * flagged (ws_cache_check, bit 1).  The attention reads code * scale rounded to
- * bf16. */
+ * bf16 (E4M3: exact); over E4M3 pages, calls of many rows take the prepared
+ * queries as the sum of two e4m3 terms, within 2^-8 of them. */
 typedef enum ws_kv_format { WS_KV_BF16 = 0, WS_KV_INT8 = 1, WS_KV_E4M3 = 2 } ws_kv_format;
 
 typedef struct ws_append_desc {
@@ -212,7 +213,8 @@ WS_API ws_status ws_cache_create(const ws_cache_config* cfg, ws_cache** out);
  * half the memory: pools of 2 * max_pages * H * 64 * 128 bytes and two fp32
  * scales per (page, head).  Its appends quantise on the way, its attention calls
  * read 8-bit pages; rows never ride in the video kernel (ws_step_attention runs
- * the two calls' kernels). */
+ * the two calls' kernels).  A call whose page list has more than 384 pages uploads
+ * it, which a capturing stream refuses (WS_ERR_UNSUPPORTED). */
 WS_API ws_status ws_cache_create_format(const ws_cache_config* cfg, ws_kv_format format, ws_cache** out);
 
 /* The format a cache was created with.  Host-only. */

