@@ -111,7 +111,8 @@ typedef struct ws_cache_config {
  * infinity, a NaN and, for INT8, a magnitude of 2^118 or more is stored as 0 and
  * flagged (ws_cache_check, bit 1).  The attention reads code * scale rounded to
  * bf16 (E4M3: exact); over E4M3 pages, calls of many rows take the prepared
- * queries as the sum of two e4m3 terms, within 2^-8 of them. */
+ * queries as sums of two e4m3 terms, within 2^-8 of themselves or 2^-21 of the row's
+ * largest (or 2^-136), whichever is more: less than the codes' own steps. */
 typedef enum ws_kv_format { WS_KV_BF16 = 0, WS_KV_INT8 = 1, WS_KV_E4M3 = 2 } ws_kv_format;
 
 typedef struct ws_append_desc {
