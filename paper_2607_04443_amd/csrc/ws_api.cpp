@@ -743,7 +743,7 @@ ws_status plan_attention(bool audio, const void* q, int64_t q_tok_stride, int64_
       } else if (window) {
         cl.n_groups = static_cast<int32_t>(ws::video_group_count(H, 1, cl.n_pages, cus));
       } else {
-        const ws::VideoTiling t = ws::video_tiling(H, cl.n_q, cl.n_pages, cus);
+        const ws::VideoTiling t = ws::video_tiling(H, cl.n_q, cl.n_pages, cus, ws::code_page_us(a.format));
         cl.tile_rows = t.rows;
         cl.n_qtiles = (cl.n_q + t.rows - 1) / t.rows;
         cl.n_groups = static_cast<int32_t>(t.groups);
@@ -852,7 +852,7 @@ void window_tiling(ws_cache* c, int32_t n_q, WindowCall* w) {
     w->few = true;
   }
   const double few_us = w->few ? few_rows_us(c, n_q, static_cast<int32_t>(c->scratch_list.size())) : -1.0;
-  const double H = c->cfg.num_heads, cus = c->num_cus;
+  const double H = c->cfg.num_heads, cus = c->num_cus, code_us = ws::code_page_us(static_cast<int32_t>(c->format));
   double best = -1.0;
   for (int rows : {256, 192, 128}) {
     const int32_t tiles = (n_q + rows - 1) / rows, mid = tiles / 2 * rows;
@@ -865,11 +865,11 @@ void window_tiling(ws_cache* c, int32_t n_q, WindowCall* w) {
     const double first = ws::video_first_us(wave_rows);
     // a round of workgroups lasts as long as one of them; from three on they even out
     const double wgs = tiles * H / cus, rounds = wgs < 3.0 ? std::ceil(wgs) : wgs + 0.5;
-    const double whole_us = rounds * (first + pages * ws::video_page_us(wave_rows, std::min(1.0, wgs)));
+    const double whole_us = rounds * (first + pages * (ws::video_page_us(wave_rows, std::min(1.0, wgs)) + code_us));
     const double units = std::min<int32_t>(tiles, ws::kMaxClasses) * H * pages, groups = std::min(cus, units);
     const double launches = (tiles + ws::kMaxClasses - 1) / ws::kMaxClasses, share = units / groups;
     const double split_us =
-        launches * (first + share * ws::video_page_us(wave_rows, groups / cus) + 5.0 * share / pages + 9.0);
+        launches * (first + share * (ws::video_page_us(wave_rows, groups / cus) + code_us) + 5.0 * share / pages + 9.0);
     for (bool whole : {false, true}) {
       const double us = whole ? whole_us : split_us;
       if (best >= 0.0 && us >= best) continue;

@@ -492,7 +492,12 @@ inline double video_page_us(int wave_rows, double load) {
   return (wave_rows == 64 ? 1.0 : wave_rows == 48 ? 0.83 : 0.6) * (0.49 + 0.96 * load);
 }
 inline double video_first_us(int wave_rows) { return wave_rows == 64 ? 14.5 : wave_rows == 48 ? 13.3 : 11.5; }
-inline double video_tiling_us(int64_t heads, int64_t n_q, int64_t pages, int64_t cus, const VideoTiling& t) {
+// What a page of 8-bit codes takes beside that, whatever the wave's rows: the conversions
+// (a window of 3680 tokens, 920 rows, 40 heads, a workgroup per head and tile of 256 /
+// 192 / 128 rows: bf16 107 / 89 / 129 us, e4m3 122 / 101 / 153, int8 137 / 122 / 197).
+inline double code_page_us(int32_t format) { return format == kFmtInt8 ? 0.47 : format == kFmtE4m3 ? 0.2 : 0.0; }
+inline double video_tiling_us(int64_t heads, int64_t n_q, int64_t pages, int64_t cus, const VideoTiling& t,
+                              double code_us = 0.0) {
   const int64_t g = t.groups, qtiles = (n_q + t.rows - 1) / t.rows;
   const int64_t one_round = cus / qtiles > 1 ? cus / qtiles : 1;
   const int64_t rounds = (g + one_round - 1) / one_round;
@@ -500,23 +505,23 @@ inline double video_tiling_us(int64_t heads, int64_t n_q, int64_t pages, int64_t
   const double segs = static_cast<double>(!split || g % heads == 0 ? (g > heads ? g : heads) : g + heads - 1) / g;
   const double load = g * qtiles < cus ? static_cast<double>(g * qtiles) / cus : 1.0;
   const int wave_rows = video_wave_rows(t.rows, static_cast<int>(n_q < t.rows ? n_q : t.rows));
-  const double page = video_page_us(wave_rows, load), first = video_first_us(wave_rows);
+  const double page = video_page_us(wave_rows, load) + code_us, first = video_first_us(wave_rows);
   const int last = static_cast<int>(n_q - (qtiles - 1) * t.rows) + kAudioQTile;
   const double audio = last > t.rows ? 5.0 : last > (kVideoWaves - 1) * video_wave_rows(t.rows, last) ? 1.0 : 0.0;
   return rounds * (static_cast<double>(heads * pages) / g * page + first + 5.0 * (segs - 1.0)) + (split ? 6.0 : 0.0) + audio;
 }
-inline VideoTiling video_tiling(int64_t heads, int64_t n_q, int64_t pages, int64_t cus) {
+inline VideoTiling video_tiling(int64_t heads, int64_t n_q, int64_t pages, int64_t cus, double code_us = 0.0) {
   auto of = [&](int rows) { return VideoTiling{rows, video_group_count(heads, (n_q + rows - 1) / rows, pages, cus)}; };
   VideoTiling best = of(kVideoQTile);
   if (pages == 0 || n_q <= kVideoQTile / 2) return best;
   const int ranges = video_max_ranges(heads, best.groups);
   const bool head_each = best.groups == heads && heads * ((n_q + kVideoQTile - 1) / kVideoQTile) <= cus;
-  double best_us = video_tiling_us(heads, n_q, pages, cus, best);
+  double best_us = video_tiling_us(heads, n_q, pages, cus, best, code_us);
   for (int rows : {192, 128}) {
     const VideoTiling t = of(rows);
     if (video_max_ranges(heads, t.groups) > ranges) continue;
     if (head_each && t.groups < heads) continue;
-    const double us = video_tiling_us(heads, n_q, pages, cus, t);
+    const double us = video_tiling_us(heads, n_q, pages, cus, t, code_us);
     if (us < best_us) {
       best = t;
       best_us = us;
