@@ -592,8 +592,9 @@ __device__ __forceinline__ void stream_start(const AttnArgs& a, VideoStream<P>& 
 // v_mfma_scale_f32_16x16x128_f8f6f4 at twice the bf16 rate.  Q'' is split into two
 // e4m3 terms of a row scale 2^f, q1 = e4m3(Q'' / 2^f) and q2 = e4m3((Q'' / 2^f - q1)
 // 16): Q'' = (q1 + q2 / 16) 2^f to within 2^-8 of itself, as one more rounding to
-// bf16 would be, or, where q2 is small, 2^-14 2^f (2^-21 of the row's largest).  The products' scale operands carry the page's K scale and the row's
-// 2^f and 2^(f - 4), so S comes out as before.  (The 128 products of an instruction
+// bf16 would be, or, where q2 is small, 2^-14 2^f (2^-21 of the row's largest).  The
+// products' scale operands carry the page's K scale and the row's 2^f and 2^(f - 4), so
+// S comes out as before.  (The 128 products of an instruction
 // are added with about 17 bits below the largest: measured against 64 bits, 3e-5 of
 // the sum of magnitudes at most on random codes of the whole range, exact on codes
 // within 2^3 of each other.)  A page of 64 rows then takes 104 MFMAs of the same total
